@@ -304,11 +304,11 @@ def _noise(s, seeds):
 def _codes(x, drop, rnd):
     """Codes of magnitudes and each block's scale."""
     x = x.view(-1, BLOCK)
-    e = x.view(torch.int32).amax(1, keepdim=True) >> 23
-    y = (x * ((253 - e) << 23).view(torch.float32) * 2.0 ** -112).view(torch.int32)
+    e = (x.view(torch.int32).amax(1, keepdim=True) - 1 >> 23) + 1  # of the power of two not below any
+    y = (x * ((254 - e) << 23).view(torch.float32) * 2.0 ** -112).view(torch.int32)
     y = (y + (rnd.view(-1, BLOCK) if torch.is_tensor(rnd) else rnd)) >> drop
-    none, bad = e < 27, e >= 253
-    scale = ((e + 1) << 23).view(torch.float32).masked_fill(none, 0.0).masked_fill(bad, math.nan)
+    none, bad = e < 28, e >= 254
+    scale = (e << 23).view(torch.float32).masked_fill(none, 0.0).masked_fill(bad, math.nan)
     return y.masked_fill(none | bad, 0).view(-1), scale.view(-1)
 
 
@@ -460,11 +460,12 @@ def _rounded(x, bits, up):
     """x with every block's magnitudes rounded to `bits` bits behind the leading one, down to 2^-14 of the scale."""
     b = x.abs().view(-1, BLOCK)
     top = b.amax(1, keepdim=True)
-    scale = torch.ldexp(torch.ones_like(top), torch.frexp(top).exponent)
+    mantissa, exponent = torch.frexp(top)
+    scale = torch.ldexp(torch.ones_like(top), exponent - (mantissa == 0.5).to(exponent.dtype))
     y = b / scale
     lsb = torch.ldexp(torch.ones_like(y), torch.clamp(torch.frexp(y).exponent - 1, min=-14) - bits)
     y = torch.floor(y / lsb + (up.view(-1, BLOCK) if torch.is_tensor(up) else up)) * lsb * scale
-    y = torch.where(top < 2.0 ** -100, 0.0, torch.where(top < 2.0 ** 126, y, math.nan))
+    y = torch.where(top <= 2.0 ** -100, 0.0, torch.where(top <= 2.0 ** 126, y, math.nan))
     return torch.copysign(y.view(-1), x)
 
 
