@@ -433,6 +433,197 @@ int fr_unpack_flagged(const fr_plan* plan, const void* payload, uint64_t payload
                       const fr_chunk_sum* sums, const uint32_t* flagged, void* dst_base,
                       uint32_t* bad_bitmap, uint64_t* n_bad, hipStream_t stream);
 
+/* ------------------------------------------------------- optimizer step */
+
+/* The step that writes the state a restore copies: one AdamW step over all
+ * tensors of the state at once (the optimizer step that the step tags of
+ * Section III-E bracket), the global norm of the gradients that scales it,
+ * the chunk sums that replicas exchange afterwards, and moments in 8 bits.
+ * The paper fixes no optimizer; the definitions below are this library's.
+ *
+ * Definitions
+ *   Arithmetic.  Every operation written below is one fp32 operation rounded
+ *     to nearest even (no fused multiply-add, denormals kept; 1 / x, / and
+ *     sqrt correctly rounded), so the new state is a function of the old one,
+ *     the gradients and the hyperparameters alone: replicas stay identical
+ *     bit for bit whatever their layouts and launch shapes.
+ *   Step.  For each element with gradient grad (bf16 or fp32), the group's
+ *     hyperparameters and the scale of the gradients (1 without stats):
+ *       g  = grad * scale
+ *       m' = beta1 * m + (1 - beta1) * g
+ *       v' = beta2 * v + (1 - beta2) * (g * g)
+ *       d  = sqrt(v') * (1 / sqrt(bias2)) + eps
+ *       w' = w * (1 - lr * weight_decay) - (m' / d) * (lr / bias1)
+ *     for the master w, and the parameter is RNE(w').
+ *   8-bit moments.  A block is FR_ADAMW_BLOCK consecutive elements of a tensor
+ *     (the last may be shorter).  Its scale is the smallest power of two that
+ *     is not below the magnitude of any element (2^(E-1) < the largest <= 2^E),
+ *     so that encoding what codes stand for gives the same codes again.
+ *       First moments: sign (bit 7), 4 exponent and 3 mantissa bits of
+ *     m / scale; second moments: 4 exponent and 4 mantissa bits of
+ *     sqrt(v) / scale (the root has the range of m, and is never negative).
+ *     A code's bits, put at bit 20 (first) or 19 (second) of an fp32 pattern,
+ *     are 2^-112 of the magnitude that it stands for, denormals included:
+ *     from 2^-17 (2^-18) of the scale up to the scale itself.  v is the square
+ *     of the root kept.
+ *       Rounding: code = (pattern(x / scale * 2^-112) + r) >> 20 (19), with
+ *     r one half of the dropped range when the seed is 0 (nearest, ties away
+ *     from zero), else h >> 12 (h & 0x7FFFF), so that the expected value is x:
+ *     second moments move by less than half a code a step, which rounding to
+ *     nearest loses.  h is a hash of the element's counter n (below), all in
+ *     32 bits: h = n * 0x9E3779B9 + seed; h ^= h >> 16; h *= 0xB504F333;
+ *     h ^= h >> 15; h *= 0x93CD3A2D; h ^= h >> 16.
+ *       A block without a magnitude above 2^-100 is kept as zeros; one that
+ *     holds a NaN, an infinity or a magnitude above 2^126 gets the scale NaN and
+ *     stands for NaN.
+ *   Counter.  Element i of tensor k has counter base_k + i, base_k the sum of
+ *     the sizes of the tensors before it, each rounded up to
+ *     FR_ADAMW_SPAN; n is its low word, with the high word times 0x85157AF5
+ *     exclusive-or'd in.
+ *   Norm.  sum_sq = the sum of the squares of all counted gradients in 64
+ *     bits, in an order that depends on the table alone; norm = sqrt(sum_sq)
+ *     rounded to fp32; scale = max_norm / norm (fp32) where norm > max_norm,
+ *     else 1; nonfinite = 1 and scale = 0 where sum_sq is not finite, else 0. */
+
+#define FR_ADAMW_BLOCK 256
+#define FR_ADAMW_SPAN 1024
+/* The smallest chunks for which fr_adamw_step writes sums. */
+#define FR_ADAMW_MIN_SUM_CHUNK 4096
+
+/* One tensor of the step: its entries in a plan's table (their src offsets
+ * and, for sums, chunks) and its gradient.  48 bytes, no padding. */
+typedef struct fr_adamw_tensor {
+  uint64_t grad_offset; /* from the gradient arena base; multiple of 16 */
+  uint32_t grad_dtype;  /* FR_F32 or FR_BF16 */
+  uint32_t group;       /* its row of the hyperparameters */
+  int32_t param;        /* FR_BF16 entry that gets RNE(master), or -1 */
+  int32_t master;       /* FR_F32 entry; its numel is the tensor's */
+  int32_t m, v;         /* FR_F32 entries: numel values each, or (8 bits)
+                           ceil(numel / 4) words that hold the codes in order */
+  int32_t m_scale;      /* -1 and -1: 32-bit moments; else FR_F32 entries of */
+  int32_t v_scale;      /* ceil(numel / FR_ADAMW_BLOCK) scales each */
+  uint32_t flags;       /* FR_GRAD_* */
+  uint32_t reserved;    /* 0 */
+} fr_adamw_tensor;
+
+/* The gradient is left out of the norm (another rank counts it: a tensor that
+ * tensor-parallel ranks hold alike). */
+#define FR_GRAD_NOT_COUNTED 1u
+
+/* Hyperparameters of a group for one step (device memory, so that a captured
+ * step replays with new ones).  32 bytes. */
+typedef struct fr_adamw_hyper {
+  float lr, beta1, beta2, eps, weight_decay;
+  float bias1, bias2; /* 1 - beta1^t and 1 - beta2^t at step t (1 and 1: no
+                         bias correction) */
+  uint32_t seed;      /* of the stochastic rounding of 8-bit moments; 0: nearest.
+                         A new one every step, the same on all replicas */
+} fr_adamw_hyper;
+
+/* What the norm leaves for the step (device memory).  24 bytes. */
+typedef struct fr_grad_stats {
+  double sum_sq;
+  float norm;
+  float scale;
+  uint64_t nonfinite; /* not 0: the step changes nothing */
+} fr_grad_stats;
+
+typedef struct fr_adamw fr_adamw; /* opaque, owned by the library */
+
+typedef struct fr_adamw_info {
+  uint64_t n_tensors;
+  uint64_t n_groups;
+  uint64_t n_elements;       /* of all tensors */
+  uint64_t n_elements_8bit;  /* of the tensors whose moments have 8 bits */
+  uint64_t n_counters;       /* the base behind the last tensor */
+  uint64_t grad_arena_bytes;
+  uint64_t arena_bytes;      /* of the state: the plan's src_arena_bytes */
+  uint64_t sums_chunks;      /* chunks whose sums a step writes (0 where the
+                                plan's chunks are below FR_ADAMW_MIN_SUM_CHUNK) */
+  int64_t device;            /* -1 for a query */
+} fr_adamw_info;
+
+/* Validate the tensors of an optimizer against a plan's table and build what
+ * its calls need on the plan's device (which must be current:
+ * FR_E_DEVICE_MISMATCH).
+ *   tensors           n descriptors (host memory; copied); order is counter order
+ *   n_groups          rows of hyperparameters that a step will be given
+ *   grad_arena_bytes  size of the gradient arena
+ * FR_E_INVAL: an index outside the table, an entry of the wrong dtype or
+ * numel, a group that does not exist, one scale without the other, unknown
+ * flags; FR_E_ALIGN: a gradient offset not a multiple of 16; FR_E_RANGE: a
+ * gradient past its arena; FR_E_OVERLAP: the src ranges of two entries that
+ * the step writes overlap, or one entry is named twice (gradients may
+ * overlap).  The plan need not outlive the optimizer.  Synchronous, like
+ * fr_plan_create; create optimizers outside graph capture. */
+int fr_adamw_create(const fr_plan* plan, const fr_adamw_tensor* tensors, uint32_t n,
+                    uint32_t n_groups, uint64_t grad_arena_bytes, fr_adamw** out);
+int fr_adamw_get_info(const fr_adamw* opt, fr_adamw_info* out);
+/* NULL is a no-op.  No work that uses it may still be pending. */
+int fr_adamw_destroy(fr_adamw* opt);
+
+/* The same validation on the host only, against a table (as fr_plan_create
+ * takes it) instead of a plan. */
+int fr_adamw_query(const fr_tensor_desc* table, uint32_t n_entries, uint64_t chunk_bytes,
+                   uint64_t arena_bytes, const fr_adamw_tensor* tensors, uint32_t n,
+                   uint32_t n_groups, uint64_t grad_arena_bytes, fr_adamw_info* info);
+
+/* A state arena laid out for an optimizer: per tensor [param bf16 (derived
+ * from the next), master, m, v], or with 8-bit moments [param, master, m codes,
+ * m scales, v codes, v scales], contiguous and 16-aligned, src and dst offsets
+ * equal; gradients of grad_dtype in order in an arena of their own.  Host only.
+ *   numel   n element counts
+ *   bits    n moment widths, 32 or 8; NULL: all 32
+ * tensors (NULL or n) gets the descriptors, group 0.  With table == NULL only
+ * the sizes are set; FR_E_RANGE if cap < *n_entries. */
+int fr_adamw_state_table(const uint64_t* numel, const uint8_t* bits, uint32_t n,
+                         uint32_t grad_dtype, fr_tensor_desc* table, uint32_t cap,
+                         uint32_t* n_entries, fr_adamw_tensor* tensors, uint64_t* arena_bytes,
+                         uint64_t* grad_bytes);
+
+/* Conventions as for the operations above: checked, then enqueued (kernel
+ * launches only, so all of it may be captured); calls on one optimizer share
+ * its scratch and must not overlap in time.  Buffers that a call reads or
+ * writes must not overlap, except where said. */
+
+/* stats <- the norm of all counted gradients and the scale that brings it to
+ * at most max_norm (> 0; infinity: scale 1).  Where ranks hold parts of the
+ * model, add up their sum_sq and call fr_grad_scale.
+ *   grads   device, 16-byte aligned, grad_arena_bytes long
+ *   stats   device, 8-byte aligned */
+int fr_grad_norm(const fr_adamw* opt, const void* grads, float max_norm, fr_grad_stats* stats,
+                 hipStream_t stream);
+
+/* norm, scale and nonfinite of stats <- from its sum_sq. */
+int fr_grad_scale(const fr_adamw* opt, float max_norm, fr_grad_stats* stats, hipStream_t stream);
+
+/* One step of all tensors.  Bytes of the arena outside their entries are not
+ * written, except that the last word of an array of codes is written whole.
+ *   state   device, 16-byte aligned, the plan's src_arena_bytes; updated
+ *   grads   device, 16-byte aligned, grad_arena_bytes long
+ *   hyper   device, 16-byte aligned, n_groups rows
+ *   stats   NULL (scale 1), or device, 8-byte aligned: with nonfinite set the
+ *           state stays as it is
+ *   sums    NULL, or device, 16-byte aligned, the plan's n_chunks entries:
+ *           those of the tensors' chunks get FRSUM-128 of the chunk after the
+ *           step (what fr_checksum_state gives for it), others are left alone;
+ *           FR_E_INVAL where the plan's chunks are below
+ *           FR_ADAMW_MIN_SUM_CHUNK bytes */
+int fr_adamw_step(const fr_adamw* opt, void* state, const void* grads,
+                  const fr_adamw_hyper* hyper, const fr_grad_stats* stats, fr_chunk_sum* sums,
+                  hipStream_t stream);
+
+/* The moments of `to` <- those of `from`, tensor by tensor, in to's forms: a
+ * rank takes over a state whose moments are kept in the other form.  Both list
+ * tensors of the same numel in the same order (FR_E_INVAL otherwise); masters,
+ * parameters and gradients are not touched.  Equal forms are copied bit for
+ * bit.
+ *   seed   of the rounding to 8 bits, as above; 0: nearest
+ * The two arenas may be the same one if no moment written lies where one is
+ * read (FR_E_OVERLAP otherwise). */
+int fr_adamw_convert(const fr_adamw* from, const void* from_state, const fr_adamw* to,
+                     void* to_state, uint32_t seed, hipStream_t stream);
+
 /* ------------------------------------------------- step tags and donors */
 
 /* Host-only controller logic that decides *which* state a restore copies and

@@ -14,7 +14,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libflashrestore.so")
-SOURCES = ["plan.cpp", "api.cpp", "steptag.cpp", "layout.cpp", "kernels.hip"]
+SOURCES = ["plan.cpp", "api.cpp", "steptag.cpp", "layout.cpp", "adamw.cpp", "kernels.hip", "adamw.hip"]
 CEIL_LIB = os.path.join(PKG, "libfrceil.so")
 CEIL_SOURCES = ["ceilings.hip"]
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")

@@ -1,0 +1,95 @@
+// Internal declarations shared by the host and device sources of the
+// optimizer step.
+#pragma once
+
+#include <cstdint>
+#include <vector>
+
+#include "flashrestore.h"
+
+namespace fr {
+
+// The arrays of a tensor whose chunks a step can sum, in this order.
+enum AdamwKind : uint32_t { kParam, kMaster, kMom1, kMom2, kScale1, kScale2, kKinds };
+constexpr uint32_t kKinds32 = kMom2 + 1;  // those of a tensor with 32-bit moments
+
+// One tensor, as the kernels read it (uniform loads).  Offsets from the state
+// arena's base, `grad` from the gradients'.
+struct alignas(16) AdamwRec {
+  uint64_t numel;
+  uint64_t counter;       // of its first element
+  uint64_t grad;
+  uint64_t at[kKinds];    // kNone: it has no such array
+  uint32_t grad_f32;
+  uint32_t group;
+  uint64_t pad_;
+};
+static_assert(sizeof(AdamwRec) == 96, "AdamwRec is 96 bytes");
+constexpr uint64_t kNone = ~uint64_t(0);
+
+// Which tile of which tensor each workgroup of a launch takes: n slots
+// (tensor << 32) | tile in order, stored XCD-major (slot g at
+// (g mod 8) * stride + g / 8).
+struct AdamwWalk {
+  const uint64_t* d = nullptr;
+  uint64_t n = 0, stride = 0;
+};
+
+// A chunk's sum: `n` consecutive slots of a walk from `slot` on, each of which
+// left its part of the array `kind`.
+struct alignas(16) AdamwFold {
+  uint32_t chunk, slot, n, kind;
+};
+
+// What the kernels of one call need of its optimizer.
+struct AdamwStepArgs {
+  const AdamwRec* recs = nullptr;
+  AdamwWalk walk;
+  bool eight = false;      // of the tensors with 8-bit moments
+  uint32_t tile = 0;       // elements a workgroup
+  void* state = nullptr;
+  const void* grads = nullptr;
+  const fr_adamw_hyper* hyper = nullptr;
+  const fr_grad_stats* stats = nullptr;  // or NULL
+  // sums, or parts == NULL
+  uint64_t C = 0;
+  fr_chunk_sum* parts = nullptr;  // walk.stride * 8 places of kKinds32 or kKinds sums
+  const AdamwFold* folds = nullptr;
+  uint32_t n_folds = 0;
+  fr_chunk_sum* sums = nullptr;
+};
+
+struct AdamwNormArgs {
+  const AdamwRec* recs = nullptr;
+  AdamwWalk walk;
+  const void* grads = nullptr;
+  float max_norm = 0;
+  fr_grad_stats* stats = nullptr;
+  double* parts = nullptr;     // kNormGroups
+  uint32_t* arrived = nullptr; // zero between calls
+};
+
+struct AdamwConvertArgs {
+  const AdamwRec* from_recs = nullptr;
+  const AdamwRec* to_recs = nullptr;
+  AdamwWalk walk;
+  bool eight = false;  // the tensors of `to` in the walk have 8-bit moments
+  const void* from = nullptr;
+  void* to = nullptr;
+  uint32_t seed = 0;
+};
+
+// Elements a workgroup takes: of a step and of a conversion, of a step that
+// also sums chunks too small for that, and of the norm.
+constexpr uint32_t kStepTile = 2048, kSmallTile = 1024, kNormTile = 8192;
+constexpr uint32_t kNormGroups = 2048;  // workgroups of a norm at most
+static_assert(kSmallTile * 4 == FR_ADAMW_MIN_SUM_CHUNK, "a tile lies inside a chunk");
+
+// Kernel launchers (adamw.hip): validated arguments, enqueue on `stream`,
+// return the hipError_t as an int.
+int launch_adamw_step(const AdamwStepArgs& a, void* stream);
+int launch_adamw_norm(const AdamwNormArgs& a, void* stream);
+int launch_adamw_scale(float max_norm, fr_grad_stats* stats, void* stream);
+int launch_adamw_convert(const AdamwConvertArgs& a, void* stream);
+
+}  // namespace fr

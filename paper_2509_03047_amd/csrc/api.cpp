@@ -9,91 +9,12 @@
 #include <new>
 #include <vector>
 
+#include "checks.h"
 #include "fr_internal.h"
-
-namespace fr {
-extern thread_local int g_last_hip_error;
-}
 
 using namespace fr;
 
 namespace {
-
-struct Region {
-  const void* p;
-  uint64_t bytes;
-};
-
-int device_error(hipError_t e) {
-  g_last_hip_error = int(e);
-  return FR_E_DEVICE;
-}
-
-int check_device_and_stream(const fr_plan* plan, hipStream_t stream) {
-  int dev = -1;
-  hipError_t e = hipGetDevice(&dev);
-  if (e != hipSuccess) return device_error(e);
-  if (dev != plan->device) return FR_E_DEVICE_MISMATCH;
-  if (stream) {
-    hipDevice_t sd = -1;
-    e = hipStreamGetDevice(hipStream_t(stream), &sd);
-    if (e != hipSuccess) {
-      (void)hipGetLastError();
-      return FR_E_INVAL;
-    }
-    if (int(sd) != plan->device) return FR_E_DEVICE_MISMATCH;
-  }
-  return FR_OK;
-}
-
-// A buffer the kernels will touch: it must be device memory of the plan's
-// device, aligned, and lie inside one allocation.  An empty buffer is never
-// touched, so any pointer (NULL included) is accepted for it.
-int check_buffer(const fr_plan* plan, const void* p, uint64_t bytes, uint64_t align) {
-  if (bytes == 0) return FR_OK;
-  if (p == nullptr) return FR_E_INVAL;
-  if (reinterpret_cast<uintptr_t>(p) % align) return FR_E_ALIGN;
-  hipPointerAttribute_t attr{};
-  hipError_t e = hipPointerGetAttributes(&attr, p);
-  if (e != hipSuccess) {
-    (void)hipGetLastError();
-    return FR_E_INVAL;  // not memory HIP knows about
-  }
-  if (attr.type != hipMemoryTypeDevice && attr.type != hipMemoryTypeManaged) return FR_E_INVAL;
-  if (attr.device != plan->device) return FR_E_DEVICE_MISMATCH;
-  hipDeviceptr_t base = nullptr;
-  size_t size = 0;
-  e = hipMemGetAddressRange(&base, &size, hipDeviceptr_t(const_cast<void*>(p)));
-  if (e != hipSuccess) {
-    (void)hipGetLastError();
-    return FR_E_INVAL;
-  }
-  const uintptr_t b = reinterpret_cast<uintptr_t>(base), q = reinterpret_cast<uintptr_t>(p);
-  if (q < b || bytes > size || q - b > size - bytes) return FR_E_RANGE;
-  return FR_OK;
-}
-
-bool overlap(const Region& x, const Region& y) {
-  if (!x.p || !y.p || x.bytes == 0 || y.bytes == 0) return false;
-  const uintptr_t a = reinterpret_cast<uintptr_t>(x.p), b = reinterpret_cast<uintptr_t>(y.p);
-  return a < b + y.bytes && b < a + x.bytes;
-}
-
-// Outputs must not overlap each other or any input.
-int check_disjoint(const Region* outs, int n_out, const Region* ins, int n_in) {
-  for (int i = 0; i < n_out; i++) {
-    for (int j = i + 1; j < n_out; j++)
-      if (overlap(outs[i], outs[j])) return FR_E_OVERLAP;
-    for (int j = 0; j < n_in; j++)
-      if (overlap(outs[i], ins[j])) return FR_E_OVERLAP;
-  }
-  return FR_OK;
-}
-
-int launch_result(int hip_rc) {
-  if (hip_rc == 0) return FR_OK;
-  return device_error(hipError_t(hip_rc));
-}
 
 // The plan's pack / checksum / compare walk at the slice size of `tile`,
 // line-aligned or not, in chunk order or (arena) in arena address order
@@ -123,12 +44,6 @@ SmallArgs small_args(const fr_plan* plan, SmallArgs::Op op) {
   return m;
 }
 
-#define FR_TRY(expr)            \
-  do {                          \
-    const int rc_ = (expr);     \
-    if (rc_ != FR_OK) return rc_; \
-  } while (0)
-
 }  // namespace
 
 extern "C" int fr_pack_state(const fr_plan* plan, const void* src_base, void* payload,
@@ -136,10 +51,10 @@ extern "C" int fr_pack_state(const fr_plan* plan, const void* src_base, void* pa
   if (!plan) return FR_E_INVAL;
   const Layout& L = plan->layout;
   if (payload_cap < L.payload_bytes) return FR_E_RANGE;
-  FR_TRY(check_device_and_stream(plan, stream));
-  FR_TRY(check_buffer(plan, src_base, plan->src_arena_bytes, 16));
-  FR_TRY(check_buffer(plan, payload, L.payload_bytes, 16));
-  FR_TRY(check_buffer(plan, sums, L.n_chunks * sizeof(fr_chunk_sum), 16));
+  FR_TRY(check_device_and_stream(plan->device, stream));
+  FR_TRY(check_buffer(plan->device, src_base, plan->src_arena_bytes, 16));
+  FR_TRY(check_buffer(plan->device, payload, L.payload_bytes, 16));
+  FR_TRY(check_buffer(plan->device, sums, L.n_chunks * sizeof(fr_chunk_sum), 16));
   const Region outs[] = {{payload, L.payload_bytes}, {sums, L.n_chunks * sizeof(fr_chunk_sum)}};
   const Region ins[] = {{src_base, plan->src_arena_bytes}};
   FR_TRY(check_disjoint(outs, 2, ins, 1));
@@ -167,12 +82,12 @@ extern "C" int fr_unpack_state(const fr_plan* plan, const void* payload, const f
   if (!plan || !n_bad) return FR_E_INVAL;
   const Layout& L = plan->layout;
   const uint64_t words = (L.n_chunks + 31) / 32;
-  FR_TRY(check_device_and_stream(plan, stream));
-  FR_TRY(check_buffer(plan, payload, L.payload_bytes, 16));
-  FR_TRY(check_buffer(plan, sums, L.n_chunks * sizeof(fr_chunk_sum), 16));
-  FR_TRY(check_buffer(plan, dst_base, plan->dst_arena_bytes, 16));
-  FR_TRY(check_buffer(plan, bad_bitmap, words * 4, 4));
-  FR_TRY(check_buffer(plan, n_bad, 8, 8));
+  FR_TRY(check_device_and_stream(plan->device, stream));
+  FR_TRY(check_buffer(plan->device, payload, L.payload_bytes, 16));
+  FR_TRY(check_buffer(plan->device, sums, L.n_chunks * sizeof(fr_chunk_sum), 16));
+  FR_TRY(check_buffer(plan->device, dst_base, plan->dst_arena_bytes, 16));
+  FR_TRY(check_buffer(plan->device, bad_bitmap, words * 4, 4));
+  FR_TRY(check_buffer(plan->device, n_bad, 8, 8));
   const Region outs[] = {{dst_base, plan->dst_arena_bytes}, {bad_bitmap, words * 4}, {n_bad, 8}};
   const Region ins[] = {{payload, L.payload_bytes}, {sums, L.n_chunks * sizeof(fr_chunk_sum)}};
   FR_TRY(check_disjoint(outs, 3, ins, 2));
@@ -225,14 +140,14 @@ int verify_checks(const fr_plan* plan, const void* base_a, const void* base_b,
   const Layout& L = plan->layout;
   const uint64_t words = (L.n_chunks + 31) / 32;
   const uint64_t sb = sums_a ? L.n_chunks * sizeof(fr_chunk_sum) : 0;
-  FR_TRY(check_device_and_stream(plan, stream));
-  FR_TRY(check_buffer(plan, base_a, plan->src_arena_bytes, 16));
-  FR_TRY(check_buffer(plan, base_b, plan->src_arena_bytes, 16));
-  FR_TRY(check_buffer(plan, diff_bitmap, words * 4, 4));
-  FR_TRY(check_buffer(plan, n_diff, 8, 8));
+  FR_TRY(check_device_and_stream(plan->device, stream));
+  FR_TRY(check_buffer(plan->device, base_a, plan->src_arena_bytes, 16));
+  FR_TRY(check_buffer(plan->device, base_b, plan->src_arena_bytes, 16));
+  FR_TRY(check_buffer(plan->device, diff_bitmap, words * 4, 4));
+  FR_TRY(check_buffer(plan->device, n_diff, 8, 8));
   if (sums_a) {
-    FR_TRY(check_buffer(plan, sums_a, sb, 16));
-    FR_TRY(check_buffer(plan, sums_b, sb, 16));
+    FR_TRY(check_buffer(plan->device, sums_a, sb, 16));
+    FR_TRY(check_buffer(plan->device, sums_b, sb, 16));
   }
   const Region outs[] = {{diff_bitmap, words * 4}, {n_diff, 8}, {sums_a, sb}, {sums_b, sb}};
   const Region ins[] = {{base_a, plan->src_arena_bytes}, {base_b, plan->src_arena_bytes}};
@@ -285,11 +200,11 @@ extern "C" int fr_compare_sums(const fr_plan* plan, const fr_chunk_sum* sums_a,
   const Layout& L = plan->layout;
   const uint64_t words = (L.n_chunks + 31) / 32;
   const uint64_t sb = L.n_chunks * sizeof(fr_chunk_sum);
-  FR_TRY(check_device_and_stream(plan, stream));
-  FR_TRY(check_buffer(plan, sums_a, sb, 16));
-  FR_TRY(check_buffer(plan, sums_b, sb, 16));
-  FR_TRY(check_buffer(plan, diff_bitmap, words * 4, 4));
-  FR_TRY(check_buffer(plan, n_diff, 8, 8));
+  FR_TRY(check_device_and_stream(plan->device, stream));
+  FR_TRY(check_buffer(plan->device, sums_a, sb, 16));
+  FR_TRY(check_buffer(plan->device, sums_b, sb, 16));
+  FR_TRY(check_buffer(plan->device, diff_bitmap, words * 4, 4));
+  FR_TRY(check_buffer(plan->device, n_diff, 8, 8));
   const Region outs[] = {{diff_bitmap, words * 4}, {n_diff, 8}};
   const Region ins[] = {{sums_a, sb}, {sums_b, sb}};
   FR_TRY(check_disjoint(outs, 2, ins, 2));
@@ -334,9 +249,9 @@ extern "C" int fr_checksum_state(const fr_plan* plan, const void* base, fr_chunk
                                  hipStream_t stream) {
   if (!plan) return FR_E_INVAL;
   const Layout& L = plan->layout;
-  FR_TRY(check_device_and_stream(plan, stream));
-  FR_TRY(check_buffer(plan, base, plan->src_arena_bytes, 16));
-  FR_TRY(check_buffer(plan, sums, L.n_chunks * sizeof(fr_chunk_sum), 16));
+  FR_TRY(check_device_and_stream(plan->device, stream));
+  FR_TRY(check_buffer(plan->device, base, plan->src_arena_bytes, 16));
+  FR_TRY(check_buffer(plan->device, sums, L.n_chunks * sizeof(fr_chunk_sum), 16));
   const Region outs[] = {{sums, L.n_chunks * sizeof(fr_chunk_sum)}};
   const Region ins[] = {{base, plan->src_arena_bytes}};
   FR_TRY(check_disjoint(outs, 1, ins, 1));
@@ -586,10 +501,10 @@ extern "C" int fr_pack_chunks(const fr_plan* plan, const void* src_base, const u
   FR_TRY(check_list(plan, ids, n_ids));
   const uint64_t pb = delta_bytes(plan, ids, n_ids);
   if (payload_cap < pb) return FR_E_RANGE;
-  FR_TRY(check_device_and_stream(plan, stream));
-  FR_TRY(check_buffer(plan, src_base, plan->src_arena_bytes, 16));
-  FR_TRY(check_buffer(plan, payload, pb, 16));
-  FR_TRY(check_buffer(plan, sums, n_ids * sizeof(fr_chunk_sum), 16));
+  FR_TRY(check_device_and_stream(plan->device, stream));
+  FR_TRY(check_buffer(plan->device, src_base, plan->src_arena_bytes, 16));
+  FR_TRY(check_buffer(plan->device, payload, pb, 16));
+  FR_TRY(check_buffer(plan->device, sums, n_ids * sizeof(fr_chunk_sum), 16));
   const Region outs[] = {{payload, pb}, {sums, n_ids * sizeof(fr_chunk_sum)}};
   const Region ins[] = {{src_base, plan->src_arena_bytes}};
   FR_TRY(check_disjoint(outs, 2, ins, 1));
@@ -608,12 +523,12 @@ extern "C" int fr_unpack_chunks(const fr_plan* plan, const void* payload, uint64
   const uint64_t pb = delta_bytes(plan, ids, n_ids);
   if (payload_bytes < pb) return FR_E_RANGE;
   const uint64_t words = (n_ids + 31) / 32;
-  FR_TRY(check_device_and_stream(plan, stream));
-  FR_TRY(check_buffer(plan, payload, pb, 16));
-  FR_TRY(check_buffer(plan, sums, n_ids * sizeof(fr_chunk_sum), 16));
-  FR_TRY(check_buffer(plan, dst_base, plan->dst_arena_bytes, 16));
-  FR_TRY(check_buffer(plan, bad_bitmap, words * 4, 4));
-  FR_TRY(check_buffer(plan, n_bad, 8, 8));
+  FR_TRY(check_device_and_stream(plan->device, stream));
+  FR_TRY(check_buffer(plan->device, payload, pb, 16));
+  FR_TRY(check_buffer(plan->device, sums, n_ids * sizeof(fr_chunk_sum), 16));
+  FR_TRY(check_buffer(plan->device, dst_base, plan->dst_arena_bytes, 16));
+  FR_TRY(check_buffer(plan->device, bad_bitmap, words * 4, 4));
+  FR_TRY(check_buffer(plan->device, n_bad, 8, 8));
   const Region outs[] = {{dst_base, plan->dst_arena_bytes}, {bad_bitmap, words * 4}, {n_bad, 8}};
   const Region ins[] = {{payload, pb}, {sums, n_ids * sizeof(fr_chunk_sum)}};
   FR_TRY(check_disjoint(outs, 3, ins, 2));
@@ -629,12 +544,12 @@ extern "C" int fr_pack_flagged(const fr_plan* plan, const void* src_base, const 
   const Layout& L = plan->layout;
   const uint64_t words = (L.n_chunks + 31) / 32, pmax = L.delta_payload_max;
   if (payload_cap < pmax) return FR_E_RANGE;
-  FR_TRY(check_device_and_stream(plan, stream));
-  FR_TRY(check_buffer(plan, src_base, plan->src_arena_bytes, 16));
-  FR_TRY(check_buffer(plan, flagged, words * 4, 4));
-  FR_TRY(check_buffer(plan, payload, pmax, 16));
-  FR_TRY(check_buffer(plan, sums, L.n_chunks * sizeof(fr_chunk_sum), 16));
-  if (counts) FR_TRY(check_buffer(plan, counts, 16, 8));
+  FR_TRY(check_device_and_stream(plan->device, stream));
+  FR_TRY(check_buffer(plan->device, src_base, plan->src_arena_bytes, 16));
+  FR_TRY(check_buffer(plan->device, flagged, words * 4, 4));
+  FR_TRY(check_buffer(plan->device, payload, pmax, 16));
+  FR_TRY(check_buffer(plan->device, sums, L.n_chunks * sizeof(fr_chunk_sum), 16));
+  if (counts) FR_TRY(check_buffer(plan->device, counts, 16, 8));
   const Region outs[] = {{payload, pmax}, {sums, L.n_chunks * sizeof(fr_chunk_sum)}, {counts, counts ? 16u : 0u}};
   const Region ins[] = {{src_base, plan->src_arena_bytes}, {flagged, words * 4}};
   FR_TRY(check_disjoint(outs, 3, ins, 2));
@@ -648,13 +563,13 @@ extern "C" int fr_unpack_flagged(const fr_plan* plan, const void* payload, uint6
   if (!plan || !n_bad) return FR_E_INVAL;
   const Layout& L = plan->layout;
   const uint64_t words = (L.n_chunks + 31) / 32;
-  FR_TRY(check_device_and_stream(plan, stream));
-  if (payload_bytes) FR_TRY(check_buffer(plan, payload, payload_bytes, 16));
-  FR_TRY(check_buffer(plan, sums, L.n_chunks * sizeof(fr_chunk_sum), 16));
-  FR_TRY(check_buffer(plan, flagged, words * 4, 4));
-  FR_TRY(check_buffer(plan, dst_base, plan->dst_arena_bytes, 16));
-  FR_TRY(check_buffer(plan, bad_bitmap, words * 4, 4));
-  FR_TRY(check_buffer(plan, n_bad, 8, 8));
+  FR_TRY(check_device_and_stream(plan->device, stream));
+  if (payload_bytes) FR_TRY(check_buffer(plan->device, payload, payload_bytes, 16));
+  FR_TRY(check_buffer(plan->device, sums, L.n_chunks * sizeof(fr_chunk_sum), 16));
+  FR_TRY(check_buffer(plan->device, flagged, words * 4, 4));
+  FR_TRY(check_buffer(plan->device, dst_base, plan->dst_arena_bytes, 16));
+  FR_TRY(check_buffer(plan->device, bad_bitmap, words * 4, 4));
+  FR_TRY(check_buffer(plan->device, n_bad, 8, 8));
   const Region outs[] = {{dst_base, plan->dst_arena_bytes}, {bad_bitmap, words * 4}, {n_bad, 8}};
   const Region ins[] = {{payload, payload_bytes}, {sums, L.n_chunks * sizeof(fr_chunk_sum)},
                         {flagged, words * 4}};

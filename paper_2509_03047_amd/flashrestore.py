@@ -37,6 +37,22 @@ DESC_DTYPE = np.dtype(
 )
 SUM_BYTES = 16  # fr_chunk_sum
 
+# fr_adamw_tensor: 48 bytes.
+ADAMW_DTYPE = np.dtype(
+    [("grad_offset", "<u8"), ("grad_dtype", "<u4"), ("group", "<u4"), ("param", "<i4"), ("master", "<i4"),
+     ("m", "<i4"), ("v", "<i4"), ("m_scale", "<i4"), ("v_scale", "<i4"), ("flags", "<u4"), ("reserved", "<u4")]
+)
+# fr_adamw_hyper: 32 bytes.
+HYPER_DTYPE = np.dtype(
+    [("lr", "<f4"), ("beta1", "<f4"), ("beta2", "<f4"), ("eps", "<f4"), ("weight_decay", "<f4"), ("bias1", "<f4"),
+     ("bias2", "<f4"), ("seed", "<u4")]
+)
+STATS_BYTES = 24  # fr_grad_stats
+FR_ADAMW_BLOCK = 256
+FR_ADAMW_SPAN = 1024
+FR_ADAMW_MIN_SUM_CHUNK = 4096
+FR_GRAD_NOT_COUNTED = 1
+
 
 class fr_plan_info(C.Structure):
     _fields_ = [
@@ -58,6 +74,14 @@ class fr_plan_info(C.Structure):
         ("tile_verify", C.c_uint32),
         ("tile_checksum", C.c_uint32),
     ]
+
+    def as_dict(self):
+        return {f: getattr(self, f) for f, _ in self._fields_}
+
+
+class fr_adamw_info(C.Structure):
+    _fields_ = [(f, C.c_uint64) for f in ("n_tensors", "n_groups", "n_elements", "n_elements_8bit", "n_counters",
+                                          "grad_arena_bytes", "arena_bytes", "sums_chunks")] + [("device", C.c_int64)]
 
     def as_dict(self):
         return {f: getattr(self, f) for f, _ in self._fields_}
@@ -118,6 +142,15 @@ def _load():
         "fr_unpack_chunks": [P, P, u64, P, P, u64, P, P, P, P],
         "fr_pack_flagged": [P, P, P, P, u64, P, P, P],
         "fr_unpack_flagged": [P, P, u64, P, P, P, P, P, P],
+        "fr_adamw_create": [P, P, u32, u32, u64, C.POINTER(P)],
+        "fr_adamw_get_info": [P, C.POINTER(fr_adamw_info)],
+        "fr_adamw_destroy": [P],
+        "fr_adamw_query": [P, u32, u64, u64, P, u32, u32, u64, C.POINTER(fr_adamw_info)],
+        "fr_adamw_state_table": [P, P, u32, u32, P, u32, C.POINTER(u32), P, C.POINTER(u64), C.POINTER(u64)],
+        "fr_grad_norm": [P, P, C.c_float, P, P],
+        "fr_grad_scale": [P, C.c_float, P, P],
+        "fr_adamw_step": [P, P, P, P, P, P, P],
+        "fr_adamw_convert": [P, P, P, P, u32, P],
         "fr_tracker_create": [u32, P, C.c_double, C.c_double, C.POINTER(P)],
         "fr_tracker_destroy": [P],
         "fr_tracker_heartbeat": [P, u32, C.c_int64, C.c_double],
@@ -150,6 +183,8 @@ EXPORTED = (
     "fr_verify_replicas", "fr_verify_replicas_noalloc", "fr_compare_sums", "fr_checksum_state",
     "fr_delta_layout",
     "fr_pack_chunks", "fr_unpack_chunks", "fr_pack_flagged", "fr_unpack_flagged",
+    "fr_adamw_create", "fr_adamw_get_info", "fr_adamw_destroy", "fr_adamw_query", "fr_adamw_state_table",
+    "fr_grad_norm", "fr_grad_scale", "fr_adamw_step", "fr_adamw_convert",
     "fr_tracker_create", "fr_tracker_destroy", "fr_tracker_heartbeat",
     "fr_tracker_report_failure", "fr_tracker_decide", "fr_tracker_failed_ranks", "fr_tracker_donors",
     "fr_layout_rank_coords", "fr_layout_donors", "fr_layout_state_table",
@@ -515,6 +550,148 @@ def fr_unpack_chunks(plan: Plan, payload, sums, chunk_ids, dst, bad_bitmap, n_ba
                                  _dev(bad_bitmap, 4 * ((ids.size + 31) // 32), "bad_bitmap"),
                                  _dev(n_bad, 8, "n_bad"), _stream(stream)), "fr_unpack_chunks")
     return _synced_bits(bad_bitmap, ids.size, stream) if sync else None
+
+
+def adamw_hyper(groups, step: int) -> np.ndarray:
+    """A fr_adamw_hyper array for step `step` (1 for the first): a dict for each
+    group, with lr and, where they differ from these, betas (0.9, 0.999), eps
+    1e-8, weight_decay 0 and seed 0 (the seed of stochastic rounding)."""
+    h = np.zeros(len(groups), HYPER_DTYPE)
+    for row, g in zip(h, groups):
+        unknown = set(g) - {"lr", "betas", "eps", "weight_decay", "seed"}
+        if unknown:
+            raise ValueError(f"unknown hyperparameters: {sorted(unknown)}")
+        b1, b2 = g.get("betas", (0.9, 0.999))
+        row["lr"], row["beta1"], row["beta2"] = g["lr"], b1, b2
+        row["eps"], row["weight_decay"], row["seed"] = g.get("eps", 1e-8), g.get("weight_decay", 0.0), g.get("seed", 0)
+        row["bias1"], row["bias2"] = 1.0 - b1 ** step, 1.0 - b2 ** step
+    return h
+
+
+def _adamw_rows(tensors) -> np.ndarray:
+    """A contiguous fr_adamw_tensor array (any structured array with these
+    fields, or rows in their order)."""
+    if isinstance(tensors, np.ndarray) and tensors.dtype.names:
+        out = np.zeros(len(tensors), dtype=ADAMW_DTYPE)
+        for f in tensors.dtype.names:
+            out[f] = tensors[f]
+        return out
+    return np.array([tuple(r) for r in tensors], dtype=ADAMW_DTYPE)
+
+
+def fr_adamw_query(table, chunk_bytes: int, arena_bytes: int, tensors, n_groups: int, grad_arena_bytes: int) -> dict:
+    """Host-only validation of an optimizer against a table: its info."""
+    t, r = as_table(table), _adamw_rows(tensors)
+    info = fr_adamw_info()
+    _check(_lib.fr_adamw_query(t.ctypes.data if len(t) else None, len(t), chunk_bytes, arena_bytes,
+                               r.ctypes.data if len(r) else None, len(r), n_groups, grad_arena_bytes,
+                               C.byref(info)), "fr_adamw_query")
+    return info.as_dict()
+
+
+def fr_adamw_state_table(numel, bits=None, grad_dtype: int = FR_BF16):
+    """(table, tensors, arena bytes, gradient arena bytes) of a state whose
+    tensors have these element counts; bits: 32 (also where None) or 8 for the
+    moments of each tensor, or one number for all."""
+    n = np.ascontiguousarray(numel, np.uint64).reshape(-1)
+    b = None if bits is None else np.ascontiguousarray(np.broadcast_to(np.asarray(bits, np.uint8), n.shape))
+    ne, ab, gb = C.c_uint32(), C.c_uint64(), C.c_uint64()
+    r = np.zeros(n.size, ADAMW_DTYPE)
+    t = np.zeros(6 * n.size, DESC_DTYPE)
+    _check(_lib.fr_adamw_state_table(n.ctypes.data if n.size else None, None if b is None else b.ctypes.data, n.size,
+                                     grad_dtype, t.ctypes.data if n.size else None, t.size, C.byref(ne),
+                                     r.ctypes.data if n.size else None, C.byref(ab), C.byref(gb)),
+           "fr_adamw_state_table")
+    return t[: ne.value], r, ab.value, gb.value
+
+
+class AdamW:
+    """An optimizer over the entries of a plan's table (``fr_adamw_*``), bound
+    to the plan's device."""
+
+    def __init__(self, plan: Plan, tensors, n_groups: int, grad_arena_bytes: int):
+        self._h = None
+        r = _adamw_rows(tensors)
+        h = C.c_void_p()
+        _check(_lib.fr_adamw_create(plan.handle, r.ctypes.data if len(r) else None, len(r), n_groups,
+                                    grad_arena_bytes, C.byref(h)), "fr_adamw_create")
+        self._h = h
+        info = fr_adamw_info()
+        _check(_lib.fr_adamw_get_info(self._h, C.byref(info)), "fr_adamw_get_info")
+        self.info = info.as_dict()
+        self.n_chunks = plan.n_chunks
+
+    @property
+    def handle(self):
+        if self._h is None:
+            raise ValueError("optimizer destroyed")
+        return self._h
+
+    def destroy(self):
+        if self._h is not None:
+            _lib.fr_adamw_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+    def empty_stats(self, device="cuda"):
+        """A fr_grad_stats as three 64-bit numbers: [0] is sum_sq, elements 2
+        and 3 of its float32 view are norm and scale, [2] of its int64 view is
+        nonfinite."""
+        import torch
+
+        return torch.empty(3, dtype=torch.float64, device=device)
+
+    def grad_norm(self, grads, max_norm, stats, stream=None):
+        return fr_grad_norm(self, grads, max_norm, stats, stream)
+
+    def grad_scale(self, max_norm, stats, stream=None):
+        return fr_grad_scale(self, max_norm, stats, stream)
+
+    def step(self, state, grads, hyper, stats=None, sums=None, stream=None):
+        return fr_adamw_step(self, state, grads, hyper, stats, sums, stream)
+
+    def convert(self, state, to: "AdamW", to_state, seed=0, stream=None):
+        return fr_adamw_convert(self, state, to, to_state, seed, stream)
+
+
+def fr_adamw_create(plan: Plan, tensors, n_groups: int, grad_arena_bytes: int) -> AdamW:
+    return AdamW(plan, tensors, n_groups, grad_arena_bytes)
+
+
+def fr_adamw_destroy(opt: AdamW) -> None:
+    opt.destroy()
+
+
+def fr_grad_norm(opt: AdamW, grads, max_norm: float, stats, stream=None) -> None:
+    _check(_lib.fr_grad_norm(opt.handle, _dev(grads, opt.info["grad_arena_bytes"], "grads"), max_norm,
+                             _dev(stats, STATS_BYTES, "stats"), _stream(stream)), "fr_grad_norm")
+
+
+def fr_grad_scale(opt: AdamW, max_norm: float, stats, stream=None) -> None:
+    _check(_lib.fr_grad_scale(opt.handle, max_norm, _dev(stats, STATS_BYTES, "stats"), _stream(stream)),
+           "fr_grad_scale")
+
+
+def fr_adamw_step(opt: AdamW, state, grads, hyper, stats=None, sums=None, stream=None) -> None:
+    """hyper: a device tensor of n_groups rows of 32 bytes (an adamw_hyper
+    array copied there); stats None: gradients as they are; sums None: none."""
+    i = opt.info
+    _check(_lib.fr_adamw_step(opt.handle, _dev(state, i["arena_bytes"], "state"),
+                              _dev(grads, i["grad_arena_bytes"], "grads"),
+                              _dev(hyper, HYPER_DTYPE.itemsize * i["n_groups"], "hyper"),
+                              _dev(stats, STATS_BYTES, "stats"), _dev(sums, SUM_BYTES * opt.n_chunks, "sums"),
+                              _stream(stream)), "fr_adamw_step")
+
+
+def fr_adamw_convert(from_opt: AdamW, from_state, to_opt: AdamW, to_state, seed: int = 0, stream=None) -> None:
+    _check(_lib.fr_adamw_convert(from_opt.handle, _dev(from_state, from_opt.info["arena_bytes"], "from_state"),
+                                 to_opt.handle, _dev(to_state, to_opt.info["arena_bytes"], "to_state"), seed,
+                                 _stream(stream)), "fr_adamw_convert")
 
 
 class Tracker:
