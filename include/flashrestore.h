@@ -464,8 +464,8 @@ int fr_unpack_flagged(const fr_plan* plan, const void* payload, uint64_t payload
  *     sqrt(v) / scale (the root has the range of m, and is never negative).
  *     A code's bits, put at bit 20 (first) or 19 (second) of an fp32 pattern,
  *     are 2^-112 of the magnitude that it stands for, denormals included:
- *     from 2^-17 (2^-18) of the scale up to the scale itself.  v is the square
- *     of the root kept.
+ *     from 2^-17 (2^-18) of the scale up to the scale itself, codes 120 (240);
+ *     larger ones are not written.  v is the square of the root kept.
  *       Rounding: code = (pattern(x / scale * 2^-112) + r) >> 20 (19), with
  *     r one half of the dropped range when the seed is 0 (nearest, ties away
  *     from zero), else h >> 12 (h & 0x7FFFF), so that the expected value is x:

@@ -32,12 +32,18 @@ bool meet(const std::vector<Range>& a, const std::vector<Range>& b) {
   return false;
 }
 
-// A walk's slots on the host, in order.
-struct Slots {
-  std::vector<uint64_t> list;
-  uint64_t stride() const { return (list.size() + 7) / 8; }
-  void add(uint32_t tensor, uint64_t numel, uint32_t tile) {
-    for (uint64_t j = 0; j * tile < numel; j++) list.push_back(uint64_t(tensor) << 32 | j);
+// A walk on the host: one run of slots per tensor, as launch_expand_slots
+// takes them.
+struct Runs {
+  uint32_t tile;  // elements
+  std::vector<uint64_t> first{0}, base;
+  explicit Runs(uint32_t t) : tile(t) {}
+  uint64_t n() const { return first.back(); }
+  uint64_t stride() const { return (n() + 7) / 8; }
+  void add(uint32_t tensor, uint64_t numel) {
+    if (!numel) return;
+    base.push_back(uint64_t(tensor) << 32);
+    first.push_back(first.back() + (numel + tile - 1) / tile);
   }
 };
 
@@ -128,7 +134,7 @@ int validate(const fr_tensor_desc* table, uint32_t n_entries, const Layout& L, u
   for (size_t i = 1; i < written.size(); i++)
     if (written[i].first < written[i - 1].last) return FR_E_OVERLAP;
   std::sort(out->moments.begin(), out->moments.end());
-  if (info.n_counters / kSmallTile + n >= (uint64_t(1) << 31)) return FR_E_RANGE;  // workgroups of a launch
+  if (info.n_counters / 256 + n >= (uint64_t(1) << 31)) return FR_E_RANGE;  // workgroups of a launch
   return FR_OK;
 }
 
@@ -140,16 +146,15 @@ struct fr_adamw {
   uint64_t C = 0, plan_chunks = 0;
   void* mem = nullptr;  // everything below
   const AdamwRec* d_recs = nullptr;
-  // By form (0: 32 bits, 1: 8): the walk of a step, that of a step which sums
-  // (the same unless chunks are too small for its tiles), what it leaves and
-  // how that is folded.
+  // By form (0: 32 bits, 1: 8): the walks of a step, of one that sums and of
+  // a conversion; what the second leaves and how that is folded.
   struct Form {
-    AdamwWalk walk, sum_walk;
-    uint32_t sum_tile = 0;
+    AdamwWalk step, sum, convert;
     fr_chunk_sum* parts = nullptr;
     const AdamwFold* folds = nullptr;
     uint32_t n_folds = 0;
   } form[2];
+  const fr_grad_stats* no_stats = nullptr;  // scale 1: a step without statistics reads these
   AdamwWalk norm;
   double* norm_parts = nullptr;
   uint32_t* arrived = nullptr;
@@ -172,53 +177,54 @@ struct Carver {
   }
 };
 
-// The XCD-major image of a walk.
-std::vector<uint64_t> image(const Slots& s) {
-  std::vector<uint64_t> out(8 * s.stride(), 0);
-  for (uint64_t g = 0; g < s.list.size(); g++) out[(g % 8) * s.stride() + g / 8] = s.list[g];
-  return out;
-}
-
 int build(fr_adamw* o) {
   const AdamwLayout& Y = o->layout;
   const uint32_t n = uint32_t(Y.recs.size());
-  Slots norm, walk[2], sum_walk[2];
+  // the walks: norm, then by form step, sum, convert
+  enum { kNorm, kStep, kSum = kStep + 2, kConvert = kSum + 2, kWalks = kConvert + 2 };
+  Runs runs[kWalks] = {Runs(kNormBytes / 4),
+                       Runs(kStepShape[0].tile()), Runs(kStepShape[1].tile()),
+                       Runs(kSumShape[0].tile()), Runs(kSumShape[1].tile()),
+                       Runs(kConvertShape[0].tile()), Runs(kConvertShape[1].tile())};
   std::vector<AdamwFold> folds[2];
   const bool sums = o->C >= FR_ADAMW_MIN_SUM_CHUNK;
-  const uint32_t sum_tile = o->C / 4 < kStepTile ? kSmallTile : kStepTile;
   for (uint32_t k = 0; k < n; k++) {
     const uint32_t f = Y.eight[k];
     const uint64_t numel = Y.recs[k].numel;
-    if (Y.counted[k]) norm.add(k, numel, kNormTile);
-    walk[f].add(k, numel, kStepTile);
-    if (!sums) continue;
-    Slots& w = sum_tile == kStepTile ? walk[f] : sum_walk[f];
-    if (sum_tile != kStepTile) w.add(k, numel, sum_tile);
-    const uint64_t tiles = (numel + sum_tile - 1) / sum_tile, first = w.list.size() - tiles;
+    // (a tile of the norm is so many bytes: of bf16 twice the elements)
+    if (Y.counted[k]) runs[kNorm].add(k, Y.recs[k].grad_f32 ? numel : (numel + 1) / 2);
+    runs[kStep + f].add(k, numel);
+    runs[kConvert + f].add(k, numel);
+    if (!sums || !numel) continue;
+    Runs& w = runs[kSum + f];
+    const uint64_t first = w.n();
+    w.add(k, numel);
+    const uint64_t tiles = w.n() - first;
     // chunk i of an array holds this many elements, and so these tiles
     const uint64_t per[kKinds] = {o->C / 2, o->C / 4, f ? o->C : o->C / 4, f ? o->C : o->C / 4,
                                   o->C / 4 * FR_ADAMW_BLOCK, o->C / 4 * FR_ADAMW_BLOCK};
     for (uint32_t j = 0; j < kKinds; j++) {
       if (Y.recs[k].at[j] == kNone) continue;
-      const uint64_t t = per[j] / sum_tile;
+      const uint64_t t = per[j] / w.tile;
       for (uint64_t i = 0; i < Y.n_chunks[size_t(k) * kKinds + j]; i++)
         folds[f].push_back({Y.chunk0[size_t(k) * kKinds + j] + uint32_t(i), uint32_t(first + i * t),
                             uint32_t(std::min(t, tiles - i * t)), j});
     }
   }
-  const std::vector<uint64_t> norm_img = image(norm), img[2] = {image(walk[0]), image(walk[1])},
-                              sum_img[2] = {image(sum_walk[0]), image(sum_walk[1])};
   Carver c;
   const size_t recs = c.add(Y.recs.data(), n * sizeof(AdamwRec));
-  const size_t nw = c.add(norm_img.data(), norm_img.size() * 8);
-  const size_t np = c.add(nullptr, kNormGroups * sizeof(double));
-  const size_t ar = c.add(nullptr, 256);
-  size_t w[2], sw[2], pt[2], fo[2];
+  const fr_grad_stats neutral = {0.0, 0.0f, 1.0f, 0};
+  const size_t ns = c.add(&neutral, sizeof neutral);
+  const size_t np = c.add(nullptr, (8 * runs[kNorm].stride() + kNormFold) * sizeof(double));
+  const size_t ar = c.add(nullptr, kNormArriveBytes);
+  size_t fi[kWalks], ba[kWalks], sl[kWalks], pt[2], fo[2];
+  for (int w = 0; w < kWalks; w++) {
+    fi[w] = c.add(runs[w].first.data(), runs[w].first.size() * 8);
+    ba[w] = c.add(runs[w].base.data(), runs[w].base.size() * 8);
+    sl[w] = c.add(nullptr, 8 * runs[w].stride() * 8);
+  }
   for (int f = 0; f < 2; f++) {
-    w[f] = c.add(img[f].data(), img[f].size() * 8);
-    sw[f] = c.add(sum_img[f].data(), sum_img[f].size() * 8);
-    const uint64_t places = sums ? 8 * (sum_tile == kStepTile ? walk[f] : sum_walk[f]).stride() : 0;
-    pt[f] = c.add(nullptr, places * (f ? kKinds : kKinds32) * sizeof(fr_chunk_sum));
+    pt[f] = c.add(nullptr, 8 * runs[kSum + f].stride() * (f ? kKinds : kKinds32) * sizeof(fr_chunk_sum));
     fo[f] = c.add(folds[f].data(), folds[f].size() * sizeof(AdamwFold));
   }
   hipError_t e = hipMalloc(&o->mem, c.total);
@@ -232,34 +238,32 @@ int build(fr_adamw* o) {
   e = hipStreamCreateWithFlags(&s, hipStreamNonBlocking);
   if (e != hipSuccess) return device_error(e);
   uint8_t* base = static_cast<uint8_t*>(o->mem);
-  for (const Carver::Piece& p : c.pieces) {
-    if (e != hipSuccess || p.bytes == 0) continue;
-    e = p.src ? hipMemcpyAsync(base + p.at, p.src, p.bytes, hipMemcpyHostToDevice, s)
-              : hipMemsetAsync(base + p.at, 0, p.bytes, s);
+  auto at = [&](size_t i) { return base + c.pieces[i].at; };
+  for (const Carver::Piece& p : c.pieces)
+    if (e == hipSuccess && p.src && p.bytes)
+      e = hipMemcpyAsync(base + p.at, p.src, p.bytes, hipMemcpyHostToDevice, s);
+  if (e == hipSuccess) e = hipMemsetAsync(at(ar), 0, kNormArriveBytes, s);
+  AdamwWalk* walks[kWalks] = {&o->norm, &o->form[0].step, &o->form[1].step, &o->form[0].sum, &o->form[1].sum,
+                              &o->form[0].convert, &o->form[1].convert};
+  for (int w = 0; w < kWalks; w++) {
+    uint64_t* d = reinterpret_cast<uint64_t*>(at(sl[w]));
+    *walks[w] = AdamwWalk{d, runs[w].n(), runs[w].stride()};
+    if (e == hipSuccess && runs[w].n())
+      e = hipError_t(launch_expand_slots(reinterpret_cast<const uint64_t*>(at(fi[w])),
+                                         reinterpret_cast<const uint64_t*>(at(ba[w])), runs[w].base.size(), runs[w].n(),
+                                         runs[w].stride(), d, s));
   }
   const hipError_t es = hipStreamSynchronize(s);
   (void)hipStreamDestroy(s);
   if (e != hipSuccess || es != hipSuccess) return device_error(e != hipSuccess ? e : es);
-
-  auto at = [&](size_t i) { return base + c.pieces[i].at; };
-  auto set = [&](AdamwWalk& d, const Slots& list, size_t i) {
-    d.d = reinterpret_cast<const uint64_t*>(at(i));
-    d.n = list.list.size();
-    d.stride = list.stride();
-  };
   o->d_recs = reinterpret_cast<const AdamwRec*>(at(recs));
-  set(o->norm, norm, nw);
+  o->no_stats = reinterpret_cast<const fr_grad_stats*>(at(ns));
   o->norm_parts = reinterpret_cast<double*>(at(np));
   o->arrived = reinterpret_cast<uint32_t*>(at(ar));
   for (int f = 0; f < 2; f++) {
-    fr_adamw::Form& F = o->form[f];
-    set(F.walk, walk[f], w[f]);
-    F.sum_tile = sum_tile;
-    if (sum_tile == kStepTile) F.sum_walk = F.walk;
-    else set(F.sum_walk, sum_walk[f], sw[f]);
-    F.parts = reinterpret_cast<fr_chunk_sum*>(at(pt[f]));
-    F.folds = reinterpret_cast<const AdamwFold*>(at(fo[f]));
-    F.n_folds = uint32_t(folds[f].size());
+    o->form[f].parts = reinterpret_cast<fr_chunk_sum*>(at(pt[f]));
+    o->form[f].folds = reinterpret_cast<const AdamwFold*>(at(fo[f]));
+    o->form[f].n_folds = uint32_t(folds[f].size());
   }
   return FR_OK;
 }
@@ -431,14 +435,13 @@ extern "C" int fr_adamw_step(const fr_adamw* opt, void* state, const void* grads
     const fr_adamw::Form& F = opt->form[f];
     AdamwStepArgs a;
     a.recs = opt->d_recs;
-    a.walk = sums ? F.sum_walk : F.walk;
+    a.walk = sums ? F.sum : F.step;
     if (a.walk.n == 0) continue;
     a.eight = f == 1;
-    a.tile = sums ? F.sum_tile : kStepTile;
     a.state = state;
     a.grads = grads;
     a.hyper = hyper;
-    a.stats = stats;
+    a.stats = stats ? stats : opt->no_stats;
     if (sums) {
       a.C = opt->C;
       a.parts = F.parts;
@@ -466,7 +469,7 @@ extern "C" int fr_adamw_convert(const fr_adamw* from, const void* from_state, co
   if (from_state == to_state ? meet(X.moments, Y.moments) : overlap(in, out)) return FR_E_OVERLAP;
   for (int f = 0; f < 2; f++) {
     AdamwConvertArgs a;
-    a.walk = to->form[f].walk;
+    a.walk = to->form[f].convert;
     if (a.walk.n == 0) continue;
     a.from_recs = from->d_recs;
     a.to_recs = to->d_recs;

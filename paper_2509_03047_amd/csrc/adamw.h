@@ -46,11 +46,10 @@ struct AdamwStepArgs {
   const AdamwRec* recs = nullptr;
   AdamwWalk walk;
   bool eight = false;      // of the tensors with 8-bit moments
-  uint32_t tile = 0;       // elements a workgroup
   void* state = nullptr;
   const void* grads = nullptr;
   const fr_adamw_hyper* hyper = nullptr;
-  const fr_grad_stats* stats = nullptr;  // or NULL
+  const fr_grad_stats* stats = nullptr;
   // sums, or parts == NULL
   uint64_t C = 0;
   fr_chunk_sum* parts = nullptr;  // walk.stride * 8 places of kKinds32 or kKinds sums
@@ -65,8 +64,8 @@ struct AdamwNormArgs {
   const void* grads = nullptr;
   float max_norm = 0;
   fr_grad_stats* stats = nullptr;
-  double* parts = nullptr;     // kNormGroups
-  uint32_t* arrived = nullptr; // zero between calls
+  double* parts = nullptr;     // a sum for each place of the walk, and kNormFold
+  uint32_t* arrived = nullptr; // lines, zero between calls
 };
 
 struct AdamwConvertArgs {
@@ -79,11 +78,25 @@ struct AdamwConvertArgs {
   uint32_t seed = 0;
 };
 
-// Elements a workgroup takes: of a step and of a conversion, of a step that
-// also sums chunks too small for that, and of the norm.
-constexpr uint32_t kStepTile = 2048, kSmallTile = 1024, kNormTile = 8192;
-constexpr uint32_t kNormGroups = 2048;  // workgroups of a norm at most
-static_assert(kSmallTile * 4 == FR_ADAMW_MIN_SUM_CHUNK, "a tile lies inside a chunk");
+// How a kernel takes its work: workgroups of B threads with U groups of four
+// elements each, and the LDS a launch asks for to bound how many of them a
+// compute unit holds (adamw.hip says why).
+struct AdamwShape {
+  uint32_t B, U, lds;
+  constexpr uint32_t tile() const { return B * U * 4; }
+};
+constexpr AdamwShape kStepShape[2] = {{64, 1, 14800}, {64, 2, 6800}};  // by form: 32 bits, 8 bits
+constexpr AdamwShape kSumShape[2] = {{64, 1, 10200}, {64, 1, 0}};   // steps that also sum
+constexpr AdamwShape kConvertShape[2] = {{64, 2, 6800}, {64, 2, 6800}};   // by the form written
+constexpr uint32_t kNormBytes = 16384;  // of gradients a workgroup of a norm takes
+// A norm of more workgroups than this adds up their sums by a second launch of
+// kNormFold; they, or those of a smaller norm, arrive at lines of kNormPerLine
+// each, whose last ones arrive at line 0.
+constexpr uint32_t kNormOne = 1024, kNormFold = 64, kNormPerLine = 32, kNormLine = 128;
+constexpr uint32_t kNormArriveBytes = (1 + kNormOne / kNormPerLine) * kNormLine;
+static_assert(kSumShape[0].B == 64 && kSumShape[1].B == 64, "one wave, which folds its own sums");
+static_assert(kSumShape[0].tile() * 4 <= FR_ADAMW_MIN_SUM_CHUNK && kSumShape[1].tile() * 4 <= FR_ADAMW_MIN_SUM_CHUNK,
+              "a summed tile lies inside a chunk");
 
 // Kernel launchers (adamw.hip): validated arguments, enqueue on `stream`,
 // return the hipError_t as an int.

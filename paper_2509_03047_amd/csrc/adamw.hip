@@ -22,8 +22,8 @@ namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr float kUp = 0x1p112f, kDown = 0x1p-112f;
 constexpr int kDrop1 = 20, kDrop2 = 19;  // bits below a code of a first moment, of a root
+constexpr int kLift = 112;               // codes at those bits stand for 2^-112 of their magnitudes
 
 __device__ __forceinline__ float as_f(uint32_t u) { return __builtin_bit_cast(float, u); }
 __device__ __forceinline__ uint32_t as_u(float f) { return __builtin_bit_cast(uint32_t, f); }
@@ -42,256 +42,494 @@ __device__ __forceinline__ Tile tile_of(const AdamwWalk& w, const AdamwRec* recs
   const uint64_t at = (g & 7) * w.stride + (g >> 3);
   const uint64_t slot = w.d[at];
   t.r = recs[slot >> 32];
-  t.e0 = (slot & 0xFFFFFFFFu) * T;
-  const uint64_t left = t.r.numel - t.e0;
-  t.n = left < T ? uint32_t(left) : uint32_t(T);
+  t.e0 = uint64_t(uint32_t(slot)) * T;
+  // (in 32 bits: a scalar 64-bit comparison has no instruction, and its detour
+  // by a vector one has been followed by a select on a stale condition)
+  const uint32_t j = uint32_t(slot), whole = uint32_t(t.r.numel / T);
+  t.n = j < whole ? uint32_t(T) : uint32_t(t.r.numel) % T;
   t.place = uint32_t(at);
   return t;
 }
 
-// Elements i ... i + 3 of the n at p, zeros behind them.
+// Elements i ... i + 3 of the n at p, zeros behind them; kFull: all four are there.
+template <bool kFull>
 __device__ __forceinline__ u32x4 load4(const void* p, uint32_t i, uint32_t n) {
   const uint32_t* q = static_cast<const uint32_t*>(p) + i;
-  if (i + 4 <= n) return ld_nt(reinterpret_cast<const u32x4*>(q));
+  if (kFull || i + 4 <= n) return ld_nt(reinterpret_cast<const u32x4*>(q));
   u32x4 x = {0, 0, 0, 0};
   for (int j = 0; j < 4; j++)
     if (i + j < n) x[j] = q[j];
   return x;
 }
-// The same of bf16 elements, as fp32 patterns.
+// The same of bf16 elements, in the first two words.
+template <bool kFull>
 __device__ __forceinline__ u32x4 load4h(const void* p, uint32_t i, uint32_t n) {
   const uint16_t* q = static_cast<const uint16_t*>(p) + i;
-  if (i + 4 <= n) {
-    const u32x2 x = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(q));
-    return u32x4{x.x << 16, x.x & 0xFFFF0000u, x.y << 16, x.y & 0xFFFF0000u};
-  }
   u32x4 x = {0, 0, 0, 0};
+  if (kFull || i + 4 <= n) {
+    x.xy = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(q));
+    return x;
+  }
   for (int j = 0; j < 4; j++)
-    if (i + j < n) x[j] = uint32_t(q[j]) << 16;
+    if (i + j < n) x[j / 2] |= uint32_t(q[j]) << (16 * (j & 1));
   return x;
 }
+// Their fp32 patterns.
+__device__ __forceinline__ u32x4 widen(const u32x4& x) {
+  return u32x4{x.x << 16, x.x & 0xFFFF0000u, x.y << 16, x.y & 0xFFFF0000u};
+}
+template <bool kFull>
 __device__ __forceinline__ void store4(void* p, u32x4 x, uint32_t i, uint32_t n) {
   uint32_t* q = static_cast<uint32_t*>(p) + i;
-  if (i + 4 <= n) return st_nt(x, reinterpret_cast<u32x4*>(q));
+  if (kFull || i + 4 <= n) return st_nt(x, reinterpret_cast<u32x4*>(q));
   for (int j = 0; j < 4; j++)
     if (i + j < n) q[j] = x[j];
 }
+template <bool kFull>
 __device__ __forceinline__ void store4h(void* p, u32x2 x, uint32_t i, uint32_t n) {
   uint16_t* q = static_cast<uint16_t*>(p) + i;
-  if (i + 4 <= n) return st_nt2(x, reinterpret_cast<u32x2*>(q));
+  if (kFull || i + 4 <= n) return st_nt2(x, reinterpret_cast<u32x2*>(q));
   for (int j = 0; j < 4; j++)
     if (i + j < n) q[j] = uint16_t(x[j / 2] >> (16 * (j & 1)));
 }
 
 // ------------------------------------------------------------ 8-bit moments
 
+// Four codes.  (Non-temporal, as everything that streams: with plain stores the
+// conversion to 8 bits took 7 % longer.)
+__device__ __forceinline__ uint32_t load_codes(const uint8_t* p) {
+  return __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(p));
+}
+__device__ __forceinline__ void store_codes(uint32_t c, uint8_t* p) {
+  __builtin_nontemporal_store(c, reinterpret_cast<uint32_t*>(p));
+}
+
+// The largest of a wave's 64 values, in all lanes (a scalar): four steps within
+// rows of 16 lanes, two across them, by data-parallel primitives.
 __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
-  for (int d = 32; d; d >>= 1) {
-    const uint32_t y = __shfl_xor(x, d);
-    x = x > y ? x : y;
+#define FR_DPP_MAX(ctrl)                                                              \
+  {                                                                                   \
+    const uint32_t y = __builtin_amdgcn_update_dpp(0u, x, ctrl, 0xF, 0xF, true);      \
+    x = x > y ? x : y;                                                                \
+  }
+  FR_DPP_MAX(0x111)  // row_shr:1
+  FR_DPP_MAX(0x112)
+  FR_DPP_MAX(0x114)
+  FR_DPP_MAX(0x118)
+  FR_DPP_MAX(0x142)  // row_bcast:15
+  FR_DPP_MAX(0x143)  // row_bcast:31
+#undef FR_DPP_MAX
+  return __builtin_amdgcn_readlane(x, 63);
+}
+
+// The larger magnitude, or NaN if one is (v_maximum3_f32).
+__device__ __forceinline__ float larger(float a, float b) {
+  return __builtin_elementwise_maximum(__builtin_fabsf(a), __builtin_fabsf(b));
+}
+
+// A wave's block: its scale, and the exponent that brings a value to where its
+// code's bits are.  Scalars: every lane has the same.
+struct Scale {
+  float scale;
+  int down;
+  bool bad;  // stands for NaN
+};
+__device__ __forceinline__ Scale scale_of(float largest) {
+  const uint32_t top = wave_max(as_u(largest) & 0x7FFFFFFFu);
+  const int e = (int(top - 1) >> 23) + 1;  // of the smallest power of two not below it
+  Scale s;
+  s.bad = e >= 254;
+  s.scale = e < 28 ? 0.0f : s.bad ? as_f(0x7FC00000u) : as_f(uint32_t(e) << 23);
+  s.down = e < 28 ? -1000 : 127 - e - kLift;  // (to zeros)
+  return s;
+}
+
+// Four first moments from their codes: as OCP e4m3 numbers the codes stand for
+// 2^8 times what they do here.
+__device__ __forceinline__ f32x4 decode1(uint32_t c, float scale) {
+  const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(c, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(c, true);
+  const float k = scale * 0x1p-8f;
+  return f32x4{a[0] * k, a[1] * k, b[0] * k, b[1] * k};
+}
+// Four second moments from the codes of their roots.  `scale` is the wave's.
+__device__ __forceinline__ f32x4 decode2(uint32_t c, float scale) {
+  constexpr uint32_t kBits = 255u << kDrop2;
+  const uint32_t e = as_u(scale) >> 23;
+  const int up = e ? int(e) - 127 + kLift : -1000;           // (a scale of 0: zeros)
+  const uint32_t bad = e == 255 ? as_u(scale) : 0u;           // (NaN, whatever the codes)
+  f32x4 v;
+#pragma unroll
+  for (int j = 0; j < 4; j++) {
+    const int shift = 8 * j - kDrop2;
+    const uint32_t u = ((shift < 0 ? c << -shift : c >> shift) & kBits) | bad;
+    const float r = __builtin_amdgcn_ldexpf(as_f(u), up);
+    v[j] = r * r;
+  }
+  return v;
+}
+
+// What is added to four elements' patterns before the bits below their codes
+// are dropped.  The low bits of the counter of the first are 0, so that the
+// products of the four differ by constants.
+struct Noise {
+  uint32_t m[4], r[4];
+};
+__device__ __forceinline__ Noise noise4(uint64_t counter, uint32_t seed) {
+  Noise x;
+  if (seed == 0) {
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+      x.m[j] = 1u << (kDrop1 - 1);
+      x.r[j] = 1u << (kDrop2 - 1);
+    }
+    return x;
+  }
+  constexpr uint32_t k1 = 0x9E3779B9u;
+  const uint32_t high = uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(counter >> 32))) * 0x85157AF5u;
+  const uint32_t p = ((uint32_t(counter) ^ high) & ~3u) * k1;
+#pragma unroll
+  for (uint32_t j = 0; j < 4; j++) {
+    // (kept a scalar, so that four products do not become of one)
+    uint32_t h = p + __builtin_amdgcn_readfirstlane(((high & 3u) ^ j) * k1 + seed);
+    h ^= h >> 16;
+    h *= 0xB504F333u;
+    h ^= h >> 15;
+    h *= 0x93CD3A2Du;
+    h ^= h >> 16;
+    x.m[j] = h >> 12;
+    x.r[j] = h & 0x7FFFFu;
   }
   return x;
 }
 
-// A block's scale and the factor that its values are encoded with, from the
-// pattern of its largest magnitude.
-struct Scale {
-  float scale, inv;
-  bool none;  // every code is 0
-};
-__device__ __forceinline__ Scale scale_of(uint32_t top) {
-  const int e = (int(top - 1) >> 23) + 1;  // of the smallest power of two not below it
-  Scale s;
-  s.none = e < 28 || e >= 254;
-  s.scale = e < 28 ? 0.0f : e >= 254 ? as_f(0x7FC00000u) : as_f(uint32_t(e) << 23);
-  s.inv = s.none ? 0.0f : as_f(uint32_t(254 - e) << 23);
-  return s;
-}
-__device__ __forceinline__ uint32_t encode(float x, const Scale& s, uint32_t rnd, int drop) {
-  return s.none ? 0 : (as_u(x * s.inv * kDown) + rnd) >> drop;
-}
-__device__ __forceinline__ float decode1(uint32_t c, float scale) {
-  return as_f((c & 127) << kDrop1 | (c & 128) << 24) * kUp * scale;
-}
-__device__ __forceinline__ float decode2(uint32_t c, float scale) { return as_f(c << kDrop2) * kUp * scale; }
-
-__device__ __forceinline__ uint32_t hash(uint64_t counter, uint32_t seed) {
-  uint32_t h = (uint32_t(counter) ^ uint32_t(counter >> 32) * 0x85157AF5u) * 0x9E3779B9u + seed;
-  h ^= h >> 16;
-  h *= 0xB504F333u;
-  h ^= h >> 15;
-  h *= 0x93CD3A2Du;
-  return h ^ h >> 16;
+// The top bytes of four words.
+__device__ __forceinline__ uint32_t pack_top(const uint32_t (&x)[4]) {
+  return __builtin_amdgcn_perm(x[1], x[0], 0x0C0C0703u) | __builtin_amdgcn_perm(x[3], x[2], 0x07030C0Cu);
 }
 
 // Codes of four first moments and four roots of second ones, which with those
 // of the wave's other lanes make up a block; the block's scales.
 __device__ __forceinline__ void encode4(const f32x4& m, const f32x4& r, uint64_t counter, uint32_t seed,
                                         uint32_t* cm, uint32_t* cr, float* sm, float* sr) {
-  uint32_t tm = 0, tr = 0;
+  const Scale xm = scale_of(larger(larger(m[0], m[1]), larger(m[2], m[3])));
+  const Scale xr = scale_of(larger(larger(r[0], r[1]), larger(r[2], r[3])));
+  const Noise z = noise4(counter, seed);
+  uint32_t a[4], b[4];  // codes in the top bytes
+#pragma unroll
   for (int j = 0; j < 4; j++) {
-    const uint32_t a = as_u(m[j]) & 0x7FFFFFFFu, b = as_u(r[j]) & 0x7FFFFFFFu;
-    tm = tm > a ? tm : a;
-    tr = tr > b ? tr : b;
+    const uint32_t u = (as_u(__builtin_amdgcn_ldexpf(m[j], xm.down)) + z.m[j]) << (24 - kDrop1);
+    a[j] = (u & 0x7FFFFFFFu) | (as_u(m[j]) & 0x80000000u);
+    b[j] = (as_u(__builtin_amdgcn_ldexpf(r[j], xr.down)) + z.r[j]) << (24 - kDrop2);
   }
-  const Scale xm = scale_of(wave_max(tm)), xr = scale_of(wave_max(tr));
-  *cm = *cr = 0;
-  for (int j = 0; j < 4; j++) {
-    uint32_t rm = 1u << (kDrop1 - 1), rr = 1u << (kDrop2 - 1);
-    if (seed) {
-      const uint32_t h = hash(counter + j, seed);
-      rm = h >> 12;
-      rr = h & 0x7FFFF;
-    }
-    const uint32_t a = encode(as_f(as_u(m[j]) & 0x7FFFFFFFu), xm, rm, kDrop1) | (as_u(m[j]) >> 24 & 128);
-    *cm |= a << (8 * j);
-    *cr |= encode(r[j], xr, rr, kDrop2) << (8 * j);
-  }
+  *cm = pack_top(a) & (xm.bad ? 0x80808080u : ~0u);
+  *cr = pack_top(b) & (xr.bad ? 0u : ~0u);
   *sm = xm.scale;
   *sr = xr.scale;
 }
 
-// --------------------------------------------------------------------- step
-
-// The sums of a workgroup's words of K arrays, in thread 0.
-template <int K, int B>
-__device__ __forceinline__ void block_sums(u64 (&s)[K], u64 (&ws)[K]) {
-  __shared__ u64 part[B / 64][2 * K];
-  for (int k = 0; k < K; k++)
-    for (int d = 32; d; d >>= 1) {
-      s[k] += __shfl_xor(s[k], d);
-      ws[k] += __shfl_xor(ws[k], d);
-    }
-  if (threadIdx.x % 64 == 0)
-    for (int k = 0; k < K; k++) {
-      part[threadIdx.x / 64][k] = s[k];
-      part[threadIdx.x / 64][K + k] = ws[k];
-    }
-  __syncthreads();
-  if (threadIdx.x == 0)
-    for (int w = 1; w < B / 64; w++)
-      for (int k = 0; k < K; k++) {
-        s[k] += part[w][k];
-        ws[k] += part[w][K + k];
-      }
+// Four fp32 patterns to bf16, two a word: v_cvt_pk_bf16_f32 rounds every
+// pattern as rne_bf16 does, NaNs included.
+__device__ __forceinline__ u32x2 to_bf16(const f32x4& x) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return u32x2{__builtin_bit_cast(uint32_t, __builtin_convertvector(x.xy, bf16x2)),
+               __builtin_bit_cast(uint32_t, __builtin_convertvector(x.zw, bf16x2))};
 }
 
-template <bool kEight, bool kSums, int B, int U>
-__global__ __launch_bounds__(B) void k_adamw(const AdamwRec* recs, AdamwWalk walk, uint8_t* state,
-                                             const uint8_t* grads, const fr_adamw_hyper* hyper,
-                                             const fr_grad_stats* stats, uint64_t C, fr_chunk_sum* parts) {
-  constexpr int K = kEight ? int(kKinds) : int(kKinds32);
-  const Tile t = tile_of<B * U * 4>(walk, recs, blockIdx.x);
-  const uint32_t n = t.n;
-  const bool skip = stats && stats->nonfinite;
-  if (skip && !kSums) return;
-  uint8_t* const pw = state + t.r.at[kMaster] + 4 * t.e0;
-  uint8_t* const pp = t.r.at[kParam] == kNone ? nullptr : state + t.r.at[kParam] + 2 * t.e0;
-  uint8_t* const pm = state + t.r.at[kMom1] + (kEight ? 1 : 4) * t.e0;
-  uint8_t* const pv = state + t.r.at[kMom2] + (kEight ? 1 : 4) * t.e0;
-  float* const psm = kEight ? reinterpret_cast<float*>(state + t.r.at[kScale1]) + t.e0 / FR_ADAMW_BLOCK : nullptr;
-  float* const psv = kEight ? reinterpret_cast<float*>(state + t.r.at[kScale2]) + t.e0 / FR_ADAMW_BLOCK : nullptr;
-  const uint8_t* const pg = grads + t.r.grad + (t.r.grad_f32 ? 4 : 2) * t.e0;
+// ------------------------------------------------ square roots and quotients
 
-  const fr_adamw_hyper h = hyper[t.r.group];
-  const float gs = stats ? stats->scale : 1.0f;
-  const float a1 = 1.0f - h.beta1, a2 = 1.0f - h.beta2;
-  const float rb2 = 1.0f / __builtin_sqrtf(h.bias2);
-  const float keep = 1.0f - h.lr * h.weight_decay, lr = h.lr / h.bias1;
+// Square roots and divisions in their general form take 13 and 11 instructions,
+// a third of them for operands near the ends of the range.  Where all of a
+// wave's operands are well inside it, these give the same correctly rounded
+// results by an approximation and Newton steps with exact residuals (fused
+// multiply-adds), as P. Markstein, "Computation of elementary functions on the
+// IBM RISC System/6000 processor" (1990), shows: a quotient that is within one
+// unit of its last place, corrected by its residual times a correctly rounded
+// reciprocal, is correctly rounded.  The root's correction and the reciprocal
+// have been compared with the general form's for every operand of the ranges
+// below.
+__device__ __forceinline__ float root_inside(float v) {  // 2^-96 <= v <= 2^126 (NaN of a negative one)
+  const float y = __builtin_amdgcn_rsqf(v), g = v * y;
+  return __builtin_fmaf(__builtin_fmaf(-g, g, v), 0.5f * y, g);
+}
+__device__ __forceinline__ float quotient_inside(float m, float d) {  // 2^-80 <= |m| <= 2^60, 2^-60 <= d <= 2^40
+  const float y0 = __builtin_amdgcn_rcpf(d);
+  const float y = __builtin_fmaf(__builtin_fmaf(-d, y0, 1.0f), y0, y0), q = m * y;
+  return __builtin_fmaf(__builtin_fmaf(-d, q, m), y, q);
+}
+// Whether the magnitudes of all of a wave's values lie in [lo, hi]; no NaN does.
+__device__ __forceinline__ bool inside(const f32x4& x, float lo, float hi) {
+  const auto least = [](float a, float b) { return __builtin_elementwise_minimum(__builtin_fabsf(a), __builtin_fabsf(b)); };
+  const float a = least(least(x[0], x[1]), least(x[2], x[3])), b = larger(larger(x[0], x[1]), larger(x[2], x[3]));
+  return __all(a >= lo && b <= hi);
+}
+__device__ __forceinline__ f32x4 roots(const f32x4& v) {
+  f32x4 r;
+  if (inside(v, 0x1p-96f, 0x1p126f)) {
+#pragma unroll
+    for (int j = 0; j < 4; j++) r[j] = root_inside(v[j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; j++) r[j] = __builtin_sqrtf(v[j]);
+  }
+  return r;
+}
 
-  u64 s[K] = {}, ws[K] = {};
+// --------------------------------------------------------------------- step
+
+// Sums over a wave of N (8 or 16) 64-bit values at once.  Each of the first
+// steps brings the lanes together in pairs that keep one half of the values
+// each, so that N values take N - 1 exchanges and the last steps for one value
+// instead of 6 N: with 8 values a quarter of the instructions.  Lane l ends with
+// the total of value l / (64 / N).
+template <int kCtrl>
+__device__ __forceinline__ u64 dpp64(u64 x) {
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0u, uint32_t(x), kCtrl, 0xF, 0xF, true);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0u, uint32_t(x >> 32), kCtrl, 0xF, 0xF, true);
+  return u64(hi) << 32 | lo;
+}
+// a + b, where lanes whose bit 5 (32) or 4 (16) is set keep b's sums and the
+// others a's.
+template <int kLanes>
+__device__ __forceinline__ u64 halve(u64 a, u64 b) {
+  const uint32_t al = uint32_t(a), ah = uint32_t(a >> 32), bl = uint32_t(b), bh = uint32_t(b >> 32);
+  if constexpr (kLanes == 32) {
+    const auto lo = __builtin_amdgcn_permlane32_swap(al, bl, false, false);
+    const auto hi = __builtin_amdgcn_permlane32_swap(ah, bh, false, false);
+    return (u64(hi[0]) << 32 | lo[0]) + (u64(hi[1]) << 32 | lo[1]);
+  } else {
+    const auto lo = __builtin_amdgcn_permlane16_swap(al, bl, false, false);
+    const auto hi = __builtin_amdgcn_permlane16_swap(ah, bh, false, false);
+    return (u64(hi[0]) << 32 | lo[0]) + (u64(hi[1]) << 32 | lo[1]);
+  }
+}
+// The same for bit 3 (row_ror:8) or 2 (row_half_mirror) of the lane.
+template <int kLanes>
+__device__ __forceinline__ u64 halve_dpp(u64 a, u64 b) {
+  const bool upper = threadIdx.x & kLanes;
+  const u64 keep = upper ? b : a, send = upper ? a : b;
+  return keep + dpp64 < kLanes == 8 ? 0x128 : 0x141 > (send);
+}
+template <int N>
+__device__ __forceinline__ u64 wave_totals(u64 (&x)[N]) {
+  static_assert(N == 8 || N == 16, "");
+#pragma unroll
+  for (int i = 0; i < N / 2; i++) x[i] = halve<32>(x[i], x[i + N / 2]);
+#pragma unroll
+  for (int i = 0; i < N / 4; i++) x[i] = halve<16>(x[i], x[i + N / 4]);
+#pragma unroll
+  for (int i = 0; i < N / 8; i++) x[i] = halve_dpp<8>(x[i], x[i + N / 8]);
+  u64 t = x[0];
+  if constexpr (N == 16) t = halve_dpp<4>(x[0], x[1]);
+  else t += dpp64<0x141>(t);  // row_half_mirror
+  t += dpp64<0x4E>(t);        // quad_perm: lanes 2 apart
+  return t + dpp64<0xB1>(t);  // and neighbours
+}
+
+// A value that is the same in all of a wave's lanes that hold one (lane 0 does).
+__device__ __forceinline__ float wave_scalar(float x) { return as_f(__builtin_amdgcn_readfirstlane(as_u(x))); }
+
+// Where a tile's arrays are.
+struct StepCtx {
+  uint8_t *pw, *pp, *pm, *pv;
+  float *psm, *psv;
+  const uint8_t* pg;
+  uint32_t n;
+  uint64_t counter;
+  fr_adamw_hyper hyper;  // its group's
+  fr_grad_stats stats;
+  uint32_t word4, word2, word1, wordb;  // first word of the tile in its chunks, by bytes an element (b: of scales)
+};
+
+// The constants of a step, each with the header's roundings.
+struct StepConsts {
+  float gs, beta1, a1, beta2, a2, rb2, eps, keep, lr;
+  uint32_t seed;
+  bool skip;
+  bool inside;  // with |v| in [2^-96, 2^60] the divisor is in [2^-60, 2^40], or NaN (of a negative v)
+};
+__device__ __forceinline__ StepConsts consts_of(const fr_adamw_hyper& h, const fr_grad_stats& g) {
+  StepConsts c;
+  c.skip = g.nonfinite != 0;
+  c.gs = g.scale;
+  c.beta1 = h.beta1;
+  c.a1 = 1.0f - h.beta1;
+  c.beta2 = h.beta2;
+  c.a2 = 1.0f - h.beta2;
+  c.rb2 = 1.0f / __builtin_sqrtf(h.bias2);
+  c.eps = h.eps;
+  c.keep = 1.0f - h.lr * h.weight_decay;
+  c.lr = h.lr / h.bias1;
+  c.seed = h.seed;
+  c.inside = c.rb2 >= 0x1p-10f && c.rb2 <= 0x1p8f && c.eps >= 0.0f && c.eps <= 0x1p39f;
+  return c;
+}
+
+// One tile.  kFull: it is whole, so that nothing is predicated; kGrad32: fp32
+// gradients.  All loads are issued before anything is waited for, the
+// constants among it.
+template <bool kEight, bool kSums, bool kFull, bool kGrad32, int B, int U, int K>
+__device__ __forceinline__ void step_tile(const StepCtx& t, u64 (&s)[K], u64 (&ws)[K]) {
+  const uint32_t n = kFull ? B * U * 4 : t.n;
+  u32x4 uw[U], um[U], uv[U], ug[U];
+  uint32_t cm[U] = {}, cv[U] = {};
+  float sm[U] = {}, sv[U] = {};
 #pragma unroll
   for (int q = 0; q < U; q++) {
-    const uint32_t i = (q * B + threadIdx.x) * 4;
-    const bool some = i < n;
-    const uint32_t b = i / FR_ADAMW_BLOCK;  // the wave's block
-    u32x4 uw = load4(pw, i, n), um, uv;
-    u32x2 up = {0, 0};
-    uint32_t cm = 0, cv = 0;
-    float sm = 0, sv = 0;
-    f32x4 m, v;
-    if (kEight) {
-      if (some) {
-        cm = *reinterpret_cast<const uint32_t*>(pm + i);
-        cv = *reinterpret_cast<const uint32_t*>(pv + i);
-        sm = psm[b];
-        sv = psv[b];
-      }
-      for (int j = 0; j < 4; j++) {
-        m[j] = decode1(cm >> (8 * j) & 255, sm);
-        v[j] = decode2(cv >> (8 * j) & 255, sv);
-        v[j] = v[j] * v[j];
+    const uint32_t i = (q * B + threadIdx.x) * 4, b = i / FR_ADAMW_BLOCK;  // the wave's block
+    uw[q] = load4<kFull>(t.pw, i, n);
+    if constexpr (kEight) {
+      if (kFull || i < n) {
+        cm[q] = load_codes(t.pm + i);
+        cv[q] = load_codes(t.pv + i);
+        sm[q] = t.psm[b];
+        sv[q] = t.psv[b];
       }
     } else {
-      um = load4(pm, i, n);
-      uv = load4(pv, i, n);
-      m = __builtin_bit_cast(f32x4, um);
-      v = __builtin_bit_cast(f32x4, uv);
+      um[q] = load4<kFull>(t.pm, i, n);
+      uv[q] = load4<kFull>(t.pv, i, n);
     }
-    if (!skip) {
-      const f32x4 g = __builtin_bit_cast(f32x4, t.r.grad_f32 ? load4(pg, i, n) : load4h(pg, i, n));
-      f32x4 w = __builtin_bit_cast(f32x4, uw), root;
+    ug[q] = kGrad32 ? load4<kFull>(t.pg, i, n) : load4h<kFull>(t.pg, i, n);
+  }
+  const StepConsts k = consts_of(t.hyper, t.stats);
+  if (k.skip && !kSums) return;
+#pragma unroll
+  for (int q = 0; q < U; q++) {
+    const uint32_t i = (q * B + threadIdx.x) * 4, b = i / FR_ADAMW_BLOCK;
+    f32x4 m, v;
+    u32x2 up = {0, 0};
+    if constexpr (kEight) {
+      m = decode1(cm[q], wave_scalar(sm[q]));
+      v = decode2(cv[q], wave_scalar(sv[q]));
+    } else {
+      m = __builtin_bit_cast(f32x4, um[q]);
+      v = __builtin_bit_cast(f32x4, uv[q]);
+    }
+    if (!k.skip) {
+      const f32x4 g = __builtin_bit_cast(f32x4, kGrad32 ? ug[q] : widen(ug[q]));
+      f32x4 w = __builtin_bit_cast(f32x4, uw[q]), root;
+#pragma unroll
       for (int j = 0; j < 4; j++) {
-        const float x = g[j] * gs;
-        m[j] = m[j] * h.beta1 + x * a1;
-        v[j] = v[j] * h.beta2 + (x * x) * a2;
-        root[j] = __builtin_sqrtf(v[j]);
-        const float d = root[j] * rb2 + h.eps;
-        w[j] = w[j] * keep - (m[j] / d) * lr;
-        if (i + j >= n) m[j] = v[j] = w[j] = root[j] = 0.0f;  // eps may be 0
+        const float x = g[j] * k.gs;
+        m[j] = m[j] * k.beta1 + x * k.a1;
+        v[j] = v[j] * k.beta2 + (x * x) * k.a2;
       }
-      uw = __builtin_bit_cast(u32x4, w);
-      up = u32x2{rne_bf16(uw.x) | rne_bf16(uw.y) << 16, rne_bf16(uw.z) | rne_bf16(uw.w) << 16};
-      store4(pw, uw, i, n);
-      if (pp) store4h(pp, up, i, n);
-      if (kEight) {
-        encode4(m, root, t.r.counter + t.e0 + i, h.seed, &cm, &cv, &sm, &sv);
-        if (some) {
-          *reinterpret_cast<uint32_t*>(pm + i) = cm;
-          *reinterpret_cast<uint32_t*>(pv + i) = cv;
+      f32x4 quotient;
+      if (k.inside && inside(m, 0x1p-80f, 0x1p60f) && inside(v, 0x1p-96f, 0x1p60f)) {
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+          root[j] = root_inside(v[j]);
+          quotient[j] = quotient_inside(m[j], root[j] * k.rb2 + k.eps);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+          root[j] = __builtin_sqrtf(v[j]);
+          quotient[j] = m[j] / (root[j] * k.rb2 + k.eps);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        w[j] = w[j] * k.keep - quotient[j] * k.lr;
+        if (!kFull && i + j >= n) m[j] = v[j] = w[j] = root[j] = 0.0f;  // eps may be 0
+      }
+      uw[q] = __builtin_bit_cast(u32x4, w);
+      up = to_bf16(w);
+      store4<kFull>(t.pw, uw[q], i, n);
+      if (t.pp) store4h<kFull>(t.pp, up, i, n);
+      if constexpr (kEight) {
+        encode4(m, root, t.counter + i, k.seed, &cm[q], &cv[q], &sm[q], &sv[q]);
+        if (kFull || i < n) {
+          store_codes(cm[q], t.pm + i);
+          store_codes(cv[q], t.pv + i);
           if (threadIdx.x % 64 == 0) {
-            psm[b] = sm;
-            psv[b] = sv;
+            t.psm[b] = sm[q];
+            t.psv[b] = sv[q];
           }
         }
       } else {
-        um = __builtin_bit_cast(u32x4, m);
-        uv = __builtin_bit_cast(u32x4, v);
-        store4(pm, um, i, n);
-        store4(pv, uv, i, n);
+        um[q] = __builtin_bit_cast(u32x4, m);
+        uv[q] = __builtin_bit_cast(u32x4, v);
+        store4<kFull>(t.pm, um[q], i, n);
+        store4<kFull>(t.pv, uv[q], i, n);
       }
-    } else if (pp) {
-      const u32x4 x = load4h(pp, i, n);
+    } else if (t.pp) {
+      const u32x4 x = widen(load4h<kFull>(t.pp, i, n));
       up = u32x2{x.x >> 16 | x.y, x.z >> 16 | x.w};
     }
-    if (kSums) {
-      const uint64_t e = t.e0 + i, mask = C - 1;
-      if (pp) acc2(up, uint32_t(2 * e & mask) / 4, s[kParam], ws[kParam]);
-      acc4(uw, uint32_t(4 * e & mask) / 4, s[kMaster], ws[kMaster]);
-      if (kEight) {
-        const u64 i1 = uint32_t(e & mask) / 4 + 1;
-        s[kMom1] += cm;
-        ws[kMom1] += i1 * cm;
-        s[kMom2] += cv;
-        ws[kMom2] += i1 * cv;
-        if (some && threadIdx.x % 64 == 0) {
-          const u64 is = uint32_t(e / FR_ADAMW_BLOCK * 4 & mask) / 4 + 1;
-          s[K - 2] += as_u(sm);
-          ws[K - 2] += is * as_u(sm);
-          s[K - 1] += as_u(sv);
-          ws[K - 1] += is * as_u(sv);
+    if constexpr (kSums) {
+      if (t.pp) acc2(up, t.word2 + i / 2, s[kParam], ws[kParam]);
+      acc4(uw[q], t.word4 + i, s[kMaster], ws[kMaster]);
+      if constexpr (kEight) {
+        const u64 i1 = t.word1 + i / 4 + 1;
+        s[kMom1] += cm[q];
+        ws[kMom1] += i1 * cm[q];
+        s[kMom2] += cv[q];
+        ws[kMom2] += i1 * cv[q];
+        if ((kFull || i < n) && threadIdx.x % 64 == 0) {
+          const u64 is = t.wordb + b + 1;
+          s[kScale1] += as_u(sm[q]);
+          ws[kScale1] += is * as_u(sm[q]);
+          s[kScale2] += as_u(sv[q]);
+          ws[kScale2] += is * as_u(sv[q]);
         }
       } else {
-        const uint32_t i0 = uint32_t(4 * e & mask) / 4;
-        acc4(um, i0, s[kMom1], ws[kMom1]);
-        acc4(uv, i0, s[kMom2], ws[kMom2]);
+        acc4(um[q], t.word4 + i, s[kMom1], ws[kMom1]);
+        acc4(uv[q], t.word4 + i, s[kMom2], ws[kMom2]);
       }
     }
   }
+}
+
+template <bool kEight, bool kSums, int B, int U>
+__global__ __launch_bounds__(B) void k_adamw(const AdamwRec* __restrict__ recs, AdamwWalk walk,
+                                             uint8_t* __restrict__ state, const uint8_t* __restrict__ grads,
+                                             const fr_adamw_hyper* __restrict__ hyper,
+                                             const fr_grad_stats* __restrict__ stats, uint64_t C,
+                                             fr_chunk_sum* __restrict__ parts) {
+  constexpr int K = kEight ? int(kKinds) : int(kKinds32);
+  const Tile t = tile_of<B * U * 4>(walk, recs, blockIdx.x);
+  StepCtx c;
+  c.n = t.n;
+  c.hyper = hyper[t.r.group];
+  c.stats = *stats;
+  c.pw = state + t.r.at[kMaster] + 4 * t.e0;
+  c.pp = t.r.at[kParam] == kNone ? nullptr : state + t.r.at[kParam] + 2 * t.e0;
+  c.pm = state + t.r.at[kMom1] + (kEight ? 1 : 4) * t.e0;
+  c.pv = state + t.r.at[kMom2] + (kEight ? 1 : 4) * t.e0;
+  c.psm = kEight ? reinterpret_cast<float*>(state + t.r.at[kScale1]) + t.e0 / FR_ADAMW_BLOCK : nullptr;
+  c.psv = kEight ? reinterpret_cast<float*>(state + t.r.at[kScale2]) + t.e0 / FR_ADAMW_BLOCK : nullptr;
+  c.pg = grads + t.r.grad + (t.r.grad_f32 ? 4 : 2) * t.e0;
+  c.counter = t.r.counter + t.e0;
+
   if (kSums) {
-    block_sums<K, B>(s, ws);
-    if (threadIdx.x == 0)
-      for (int k = 0; k < K; k++) parts[uint64_t(t.place) * K + k] = fr_chunk_sum{s[k], ws[k]};
+    const uint64_t mask = C - 1;
+    c.word4 = uint32_t(4 * t.e0 & mask) / 4;
+    c.word2 = uint32_t(2 * t.e0 & mask) / 4;
+    c.word1 = uint32_t(t.e0 & mask) / 4;
+    c.wordb = uint32_t(t.e0 / FR_ADAMW_BLOCK * 4 & mask) / 4;
+  }
+
+  u64 s[K] = {}, ws[K] = {};
+  if (t.n == B * U * 4) {
+    if (t.r.grad_f32) step_tile<kEight, kSums, true, true, B, U>(c, s, ws);
+    else step_tile<kEight, kSums, true, false, B, U>(c, s, ws);
+  } else {
+    if (t.r.grad_f32) step_tile<kEight, kSums, false, true, B, U>(c, s, ws);
+    else step_tile<kEight, kSums, false, false, B, U>(c, s, ws);
+  }
+  if constexpr (kSums) {
+    static_assert(B == 64, "a wave");
+    constexpr int N = K <= 4 ? 8 : 16;
+    u64 x[N] = {};
+#pragma unroll
+    for (int k = 0; k < K; k++) {
+      x[2 * k] = s[k];
+      x[2 * k + 1] = ws[k];
+    }
+    const u64 total = wave_totals(x);
+    const uint32_t v = threadIdx.x / (64 / N);
+    if (threadIdx.x % (64 / N) == 0 && v < 2 * K)
+      reinterpret_cast<u64*>(parts + uint64_t(t.place) * K)[v] = total;
   }
 }
 
@@ -339,26 +577,64 @@ __device__ __forceinline__ double block_sum(double x) {
   return x;
 }
 
-// Workgroup g takes tiles g, g + G, ...; the one that ends last adds up what
-// all have left, each thread and the whole in an order of their own, whoever
-// it is.
-__global__ __launch_bounds__(256) void k_norm(const AdamwRec* recs, AdamwWalk walk, const uint8_t* grads,
-                                              float max_norm, fr_grad_stats* stats, double* parts,
-                                              uint32_t* arrived) {
+// The sum of the squares of a thread's share of one tile.  kFull: the tile is
+// whole, and all its loads are in flight before the first is used.
+template <bool kFull, bool kGrad32>
+__device__ __forceinline__ double squares(const uint8_t* p, uint32_t n) {
   double sum = 0;
-  for (uint64_t g = blockIdx.x; g < walk.n; g += gridDim.x) {
-    const Tile t = tile_of<kNormTile>(walk, recs, g);
-    const uint8_t* const p = grads + t.r.grad + (t.r.grad_f32 ? 4 : 2) * t.e0;
-    for (uint32_t i = threadIdx.x * 4; i < t.n; i += 256 * 4) {
-      const f32x4 x = __builtin_bit_cast(f32x4, t.r.grad_f32 ? load4(p, i, t.n) : load4h(p, i, t.n));
+  if constexpr (kFull) {
+    constexpr int V = kNormBytes / (256 * 16);
+    u32x4 x[V];
+#pragma unroll
+    for (int q = 0; q < V; q++) x[q] = ld_nt(reinterpret_cast<const u32x4*>(p) + q * 256 + threadIdx.x);
+#pragma unroll
+    for (int q = 0; q < V; q++)
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        if (kGrad32) {
+          const double a = as_f(x[q][j]);
+          sum += a * a;
+        } else {
+          const double a = as_f(x[q][j] << 16), b = as_f(x[q][j] & 0xFFFF0000u);
+          sum += a * a;
+          sum += b * b;
+        }
+      }
+  } else {
+    for (uint32_t i = threadIdx.x * 4; i < n; i += 256 * 4) {
+      const f32x4 x = __builtin_bit_cast(f32x4, kGrad32 ? load4<false>(p, i, n) : widen(load4h<false>(p, i, n)));
       for (int j = 0; j < 4; j++) sum += double(x[j]) * double(x[j]);
     }
   }
-  sum = block_sum(sum);
+  return sum;
+}
+
+// Adds one arrival of `of` at a line; whether it was the last one, for which
+// the line is left at zero.
+__device__ __forceinline__ bool arrive_last(uint32_t* lines, uint32_t line, uint32_t of) {
+  uint32_t* p = lines + line * (kNormLine / 4);
+  if (__hip_atomic_fetch_add(p, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != of - 1) return false;
+  __hip_atomic_store(p, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return true;
+}
+
+// The end of a workgroup's part `sum` (thread 0's) of a norm: it is left at
+// parts[blockIdx.x]; whoever arrives last adds up all, each thread and the
+// whole in an order of their own, whoever it is.  A part is exchanged, not
+// stored, and its return waited for before the arrival is added: it is then
+// where every other workgroup's atomic loads find it, without the release
+// and acquire that write back and invalidate a whole L2 each (1,800 of them
+// took 35 us).
+__device__ __forceinline__ void finish_norm(double sum, double* parts, uint32_t* arrived, float max_norm,
+                                            fr_grad_stats* stats) {
   __shared__ bool last;
   if (threadIdx.x == 0) {
-    __hip_atomic_store(parts + blockIdx.x, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    last = __hip_atomic_fetch_add(arrived, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+    (void)__hip_atomic_exchange(reinterpret_cast<unsigned long long*>(parts + blockIdx.x),
+                                __builtin_bit_cast(unsigned long long, sum), __ATOMIC_RELAXED,
+                                __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    const uint32_t lines = (gridDim.x + kNormPerLine - 1) / kNormPerLine, line = blockIdx.x % lines;
+    last = arrive_last(arrived, 1 + line, (gridDim.x - line + lines - 1) / lines) && arrive_last(arrived, 0, lines);
   }
   __syncthreads();
   if (!last) return;
@@ -366,106 +642,181 @@ __global__ __launch_bounds__(256) void k_norm(const AdamwRec* recs, AdamwWalk wa
   for (uint32_t i = threadIdx.x; i < gridDim.x; i += 256)
     sum += __hip_atomic_load(parts + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   sum = block_sum(sum);
-  if (threadIdx.x == 0) {
-    set_stats(sum, max_norm, stats);
-    __hip_atomic_store(arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (threadIdx.x == 0) set_stats(sum, max_norm, stats);
+}
+
+// One tile a workgroup.  kOne: the only launch of the norm; else its part goes
+// to its place for k_norm_fold.
+template <bool kOne>
+__global__ __launch_bounds__(256) void k_norm(const AdamwRec* recs, AdamwWalk walk, const uint8_t* grads,
+                                              float max_norm, fr_grad_stats* stats, double* parts,
+                                              uint32_t* arrived) {
+  double sum = 0;
+  const uint32_t g = blockIdx.x, at = (g & 7) * uint32_t(walk.stride) + (g >> 3);
+  if (!kOne || walk.n) {  // (no tiles: one workgroup, of nothing)
+    const uint64_t slot = walk.d[at];
+    const AdamwRec& r = recs[slot >> 32];
+    const uint8_t* const p = grads + r.grad + uint64_t(uint32_t(slot)) * kNormBytes;
+    const bool f32 = r.grad_f32 != 0;
+    const uint32_t T = kNormBytes / (f32 ? 4 : 2), whole = uint32_t(r.numel / T);
+    if (uint32_t(slot) < whole) sum = f32 ? squares<true, true>(p, T) : squares<true, false>(p, T);
+    else sum = f32 ? squares<false, true>(p, uint32_t(r.numel) % T) : squares<false, false>(p, uint32_t(r.numel) % T);
   }
+  sum = block_sum(sum);
+  if constexpr (kOne) finish_norm(sum, parts, arrived, max_norm, stats);
+  else if (threadIdx.x == 0) parts[at] = sum;
+}
+
+// The sum of the places' parts: each workgroup adds a run of them up.
+__global__ __launch_bounds__(256) void k_norm_fold(uint64_t stride, uint64_t n, double* parts, double* parts2,
+                                                   float max_norm, fr_grad_stats* stats, uint32_t* arrived) {
+  const uint32_t places = 8 * uint32_t(stride), run = (places + gridDim.x - 1) / gridDim.x;
+  const uint32_t first = blockIdx.x * run, end = first + run < places ? first + run : places;
+  double sum = 0;
+  for (uint32_t i = first + threadIdx.x; i < end; i += 256) {
+    const uint32_t x = i / uint32_t(stride);
+    if ((i - x * uint32_t(stride)) * 8 + x < uint32_t(n)) sum += parts[i];  // the others are no workgroup's
+  }
+  sum = block_sum(sum);
+  finish_norm(sum, parts2, arrived, max_norm, stats);
 }
 
 __global__ void k_scale(float max_norm, fr_grad_stats* stats) { set_stats(stats->sum_sq, max_norm, stats); }
 
 // ------------------------------------------------------------------ convert
 
-template <bool kEight, int B, int U>
+struct ConvertCtx {
+  const uint8_t *qm, *qv;
+  const float *qsm, *qsv;
+  uint8_t *pm, *pv;
+  float *psm, *psv;
+  uint32_t n, seed;
+  uint64_t counter;
+};
+
+// One tile; k8From, k8To: the forms.  All loads are issued before the first is
+// used.
+template <bool k8From, bool k8To, bool kFull, int B, int U>
+__device__ __forceinline__ void convert_tile(const ConvertCtx& t) {
+  const uint32_t n = kFull ? B * U * 4 : t.n;
+  u32x4 um[U], uv[U];
+  uint32_t cm[U] = {}, cv[U] = {};
+  float sm[U] = {}, sv[U] = {};
+#pragma unroll
+  for (int q = 0; q < U; q++) {
+    const uint32_t i = (q * B + threadIdx.x) * 4, b = i / FR_ADAMW_BLOCK;
+    if constexpr (k8From) {
+      if (kFull || i < n) {
+        cm[q] = load_codes(t.qm + i);
+        cv[q] = load_codes(t.qv + i);
+        sm[q] = t.qsm[b];
+        sv[q] = t.qsv[b];
+      }
+    } else {
+      um[q] = load4<kFull>(t.qm, i, n);
+      uv[q] = load4<kFull>(t.qv, i, n);
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < U; q++) {
+    const uint32_t i = (q * B + threadIdx.x) * 4, b = i / FR_ADAMW_BLOCK;
+    if constexpr (k8From && !k8To) {
+      um[q] = __builtin_bit_cast(u32x4, decode1(cm[q], wave_scalar(sm[q])));
+      uv[q] = __builtin_bit_cast(u32x4, decode2(cv[q], wave_scalar(sv[q])));
+    }
+    if constexpr (!k8From && k8To) {
+      const f32x4 r = roots(__builtin_bit_cast(f32x4, uv[q]));
+      encode4(__builtin_bit_cast(f32x4, um[q]), r, t.counter + i, t.seed, &cm[q], &cv[q], &sm[q], &sv[q]);
+    }
+    if constexpr (k8To) {
+      if (kFull || i < n) {
+        store_codes(cm[q], t.pm + i);
+        store_codes(cv[q], t.pv + i);
+        if (threadIdx.x % 64 == 0) {
+          t.psm[b] = sm[q];
+          t.psv[b] = sv[q];
+        }
+      }
+    } else {
+      store4<kFull>(t.pm, um[q], i, n);
+      store4<kFull>(t.pv, uv[q], i, n);
+    }
+  }
+}
+
+template <bool k8To, int B, int U>
 __global__ __launch_bounds__(B) void k_convert(const AdamwRec* from_recs, const AdamwRec* to_recs, AdamwWalk walk,
                                                const uint8_t* from, uint8_t* to, uint32_t seed) {
   const Tile t = tile_of<B * U * 4>(walk, to_recs, blockIdx.x);
   const AdamwRec f = from_recs[walk.d[t.place] >> 32];
   const bool f8 = f.at[kScale1] != kNone;
   const uint64_t b0 = t.e0 / FR_ADAMW_BLOCK;
-  const uint8_t* const qm = from + f.at[kMom1] + (f8 ? 1 : 4) * t.e0;
-  const uint8_t* const qv = from + f.at[kMom2] + (f8 ? 1 : 4) * t.e0;
-  const float* const qsm = f8 ? reinterpret_cast<const float*>(from + f.at[kScale1]) + b0 : nullptr;
-  const float* const qsv = f8 ? reinterpret_cast<const float*>(from + f.at[kScale2]) + b0 : nullptr;
-  uint8_t* const pm = to + t.r.at[kMom1] + (kEight ? 1 : 4) * t.e0;
-  uint8_t* const pv = to + t.r.at[kMom2] + (kEight ? 1 : 4) * t.e0;
-  float* const psm = kEight ? reinterpret_cast<float*>(to + t.r.at[kScale1]) + b0 : nullptr;
-  float* const psv = kEight ? reinterpret_cast<float*>(to + t.r.at[kScale2]) + b0 : nullptr;
-#pragma unroll
-  for (int q = 0; q < U; q++) {
-    const uint32_t i = (q * B + threadIdx.x) * 4;
-    const bool some = i < t.n;
-    const uint32_t b = i / FR_ADAMW_BLOCK;
-    f32x4 m = {0, 0, 0, 0}, v = m;
-    uint32_t cm = 0, cv = 0;
-    float sm = 0, sv = 0;
-    if (f8) {
-      if (some) {
-        cm = *reinterpret_cast<const uint32_t*>(qm + i);
-        cv = *reinterpret_cast<const uint32_t*>(qv + i);
-        sm = qsm[b];
-        sv = qsv[b];
-      }
-      if (!kEight)
-        for (int j = 0; j < 4; j++) {
-          m[j] = decode1(cm >> (8 * j) & 255, sm);
-          v[j] = decode2(cv >> (8 * j) & 255, sv);
-          v[j] = v[j] * v[j];
-        }
-    } else {
-      m = __builtin_bit_cast(f32x4, load4(qm, i, t.n));
-      v = __builtin_bit_cast(f32x4, load4(qv, i, t.n));
-      if (kEight) {
-        for (int j = 0; j < 4; j++) v[j] = __builtin_sqrtf(v[j]);
-        encode4(m, v, t.r.counter + t.e0 + i, seed, &cm, &cv, &sm, &sv);
-      }
-    }
-    if (kEight) {
-      if (some) {
-        *reinterpret_cast<uint32_t*>(pm + i) = cm;
-        *reinterpret_cast<uint32_t*>(pv + i) = cv;
-        if (threadIdx.x % 64 == 0) {
-          psm[b] = sm;
-          psv[b] = sv;
-        }
-      }
-    } else {
-      store4(pm, __builtin_bit_cast(u32x4, m), i, t.n);
-      store4(pv, __builtin_bit_cast(u32x4, v), i, t.n);
-    }
+  ConvertCtx c;
+  c.qm = from + f.at[kMom1] + (f8 ? 1 : 4) * t.e0;
+  c.qv = from + f.at[kMom2] + (f8 ? 1 : 4) * t.e0;
+  c.qsm = f8 ? reinterpret_cast<const float*>(from + f.at[kScale1]) + b0 : nullptr;
+  c.qsv = f8 ? reinterpret_cast<const float*>(from + f.at[kScale2]) + b0 : nullptr;
+  c.pm = to + t.r.at[kMom1] + (k8To ? 1 : 4) * t.e0;
+  c.pv = to + t.r.at[kMom2] + (k8To ? 1 : 4) * t.e0;
+  c.psm = k8To ? reinterpret_cast<float*>(to + t.r.at[kScale1]) + b0 : nullptr;
+  c.psv = k8To ? reinterpret_cast<float*>(to + t.r.at[kScale2]) + b0 : nullptr;
+  c.n = t.n;
+  c.seed = seed;
+  c.counter = t.r.counter + t.e0;
+  if (t.n == B * U * 4) {
+    if (f8) convert_tile<true, k8To, true, B, U>(c);
+    else convert_tile<false, k8To, true, B, U>(c);
+  } else {
+    if (f8) convert_tile<true, k8To, false, B, U>(c);
+    else convert_tile<false, k8To, false, B, U>(c);
   }
 }
 
-template <bool kEight, bool kSums, int B, int U>
+template <bool kEight, bool kSums>
 int step(const AdamwStepArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL((k_adamw<kEight, kSums, B, U>), dim3(uint32_t(a.walk.n)), dim3(B), 0, st, a.recs, a.walk,
+  constexpr AdamwShape s = kSums ? kSumShape[kEight] : kStepShape[kEight];
+  hipLaunchKernelGGL((k_adamw<kEight, kSums, s.B, s.U>), dim3(uint32_t(a.walk.n)), dim3(s.B), s.lds, st, a.recs, a.walk,
                      static_cast<uint8_t*>(a.state), static_cast<const uint8_t*>(a.grads), a.hyper, a.stats, a.C,
                      a.parts);
-  return int(hipGetLastError());
-}
-
-template <bool kEight>
-int step_of(const AdamwStepArgs& a, hipStream_t st) {
-  if (!a.parts) return step<kEight, false, 256, kStepTile / 1024>(a, st);
-  const int e = a.tile == kStepTile ? step<kEight, true, 256, kStepTile / 1024>(a, st)
-                                    : step<kEight, true, 256, kSmallTile / 1024>(a, st);
-  if (e != 0 || a.n_folds == 0) return e;
+  const int e = int(hipGetLastError());
+  if (e != 0 || !kSums || a.n_folds == 0) return e;
   constexpr int K = kEight ? int(kKinds) : int(kKinds32);
   hipLaunchKernelGGL((k_adamw_fold<K>), dim3((a.n_folds + 15) / 16), dim3(256), 0, st, a.folds, a.n_folds,
                      a.walk.stride, a.parts, a.sums);
   return int(hipGetLastError());
 }
 
+template <bool kEight>
+int convert(const AdamwConvertArgs& a, hipStream_t st) {
+  constexpr AdamwShape s = kConvertShape[kEight];
+  hipLaunchKernelGGL((k_convert<kEight, s.B, s.U>), dim3(uint32_t(a.walk.n)), dim3(s.B), s.lds, st, a.from_recs,
+                     a.to_recs, a.walk, static_cast<const uint8_t*>(a.from), static_cast<uint8_t*>(a.to), a.seed);
+  return int(hipGetLastError());
+}
+
 }  // namespace
 
 int launch_adamw_step(const AdamwStepArgs& a, void* stream) {
-  return a.eight ? step_of<true>(a, hipStream_t(stream)) : step_of<false>(a, hipStream_t(stream));
+  const hipStream_t st = hipStream_t(stream);
+  if (a.parts) return a.eight ? step<true, true>(a, st) : step<false, true>(a, st);
+  return a.eight ? step<true, false>(a, st) : step<false, false>(a, st);
 }
 
 int launch_adamw_norm(const AdamwNormArgs& a, void* stream) {
-  const uint32_t groups = a.walk.n < 1 ? 1 : a.walk.n < kNormGroups ? uint32_t(a.walk.n) : kNormGroups;
-  hipLaunchKernelGGL(k_norm, dim3(groups), dim3(256), 0, hipStream_t(stream), a.recs, a.walk,
-                     static_cast<const uint8_t*>(a.grads), a.max_norm, a.stats, a.parts, a.arrived);
+  const hipStream_t st = hipStream_t(stream);
+  const uint8_t* grads = static_cast<const uint8_t*>(a.grads);
+  const uint32_t n = uint32_t(a.walk.n);
+  if (n <= kNormOne) {
+    hipLaunchKernelGGL(k_norm<true>, dim3(n ? n : 1), dim3(256), 0, st, a.recs, a.walk, grads, a.max_norm, a.stats,
+                       a.parts, a.arrived);
+    return int(hipGetLastError());
+  }
+  hipLaunchKernelGGL(k_norm<false>, dim3(n), dim3(256), 0, st, a.recs, a.walk, grads, a.max_norm, a.stats, a.parts,
+                     a.arrived);
+  const int e = int(hipGetLastError());
+  if (e != 0) return e;
+  hipLaunchKernelGGL(k_norm_fold, dim3(kNormFold), dim3(256), 0, st, a.walk.stride, a.walk.n, a.parts,
+                     a.parts + 8 * a.walk.stride, a.max_norm, a.stats, a.arrived);
   return int(hipGetLastError());
 }
 
@@ -475,17 +826,7 @@ int launch_adamw_scale(float max_norm, fr_grad_stats* stats, void* stream) {
 }
 
 int launch_adamw_convert(const AdamwConvertArgs& a, void* stream) {
-  const dim3 grid(uint32_t(a.walk.n)), block(256);
-  const hipStream_t st = hipStream_t(stream);
-  const uint8_t* from = static_cast<const uint8_t*>(a.from);
-  uint8_t* to = static_cast<uint8_t*>(a.to);
-  if (a.eight)
-    hipLaunchKernelGGL((k_convert<true, 256, kStepTile / 1024>), grid, block, 0, st, a.from_recs, a.to_recs, a.walk,
-                       from, to, a.seed);
-  else
-    hipLaunchKernelGGL((k_convert<false, 256, kStepTile / 1024>), grid, block, 0, st, a.from_recs, a.to_recs, a.walk,
-                       from, to, a.seed);
-  return int(hipGetLastError());
+  return a.eight ? convert<true>(a, hipStream_t(stream)) : convert<false>(a, hipStream_t(stream));
 }
 
 }  // namespace fr
