@@ -87,12 +87,14 @@ struct AdamwShape {
 };
 constexpr AdamwShape kStepShape[2] = {{64, 1, 14800}, {64, 2, 6800}};  // by form: 32 bits, 8 bits
 constexpr AdamwShape kSumShape[2] = {{64, 1, 10200}, {64, 1, 0}};   // steps that also sum
-constexpr AdamwShape kConvertShape[2] = {{64, 2, 6800}, {64, 2, 6800}};   // by the form written
+constexpr AdamwShape kConvertShape[2] = {{64, 8, 32000}, {128, 2, 13500}};   // by the form written
 constexpr uint32_t kNormBytes = 16384;  // of gradients a workgroup of a norm takes
 // A norm of more workgroups than this adds up their sums by a second launch of
 // kNormFold; they, or those of a smaller norm, arrive at lines of kNormPerLine
 // each, whose last ones arrive at line 0.
-constexpr uint32_t kNormOne = 1024, kNormFold = 64, kNormPerLine = 32, kNormLine = 128;
+// (up to kNormOneLine at line 0 themselves: arrivals at one line take 7 ns each,
+// another line a round trip).
+constexpr uint32_t kNormOne = 1024, kNormFold = 64, kNormPerLine = 32, kNormOneLine = 64, kNormLine = 128;
 constexpr uint32_t kNormArriveBytes = (1 + kNormOne / kNormPerLine) * kNormLine;
 static_assert(kSumShape[0].B == 64 && kSumShape[1].B == 64, "one wave, which folds its own sums");
 static_assert(kSumShape[0].tile() * 4 <= FR_ADAMW_MIN_SUM_CHUNK && kSumShape[1].tile() * 4 <= FR_ADAMW_MIN_SUM_CHUNK,

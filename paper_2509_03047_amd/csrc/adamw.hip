@@ -634,7 +634,9 @@ __device__ __forceinline__ void finish_norm(double sum, double* parts, uint32_t*
                                 __HIP_MEMORY_SCOPE_AGENT);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     const uint32_t lines = (gridDim.x + kNormPerLine - 1) / kNormPerLine, line = blockIdx.x % lines;
-    last = arrive_last(arrived, 1 + line, (gridDim.x - line + lines - 1) / lines) && arrive_last(arrived, 0, lines);
+    last = gridDim.x <= kNormOneLine
+               ? arrive_last(arrived, 0, gridDim.x)
+               : arrive_last(arrived, 1 + line, (gridDim.x - line + lines - 1) / lines) && arrive_last(arrived, 0, lines);
   }
   __syncthreads();
   if (!last) return;

@@ -237,10 +237,14 @@ def _dev(x, need: int, name: str) -> int | None:
 
 
 def _stream(stream) -> int | None:
+    """A stream's handle; None is the current stream (asked for by its handle:
+    the stream object takes 2.5 us to make, as long as a small kernel runs)."""
     if stream is None:
         import torch
 
-        return torch.cuda.current_stream().cuda_stream or None
+        if not torch.cuda.is_initialized():
+            torch.cuda.init()
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) or None
     if isinstance(stream, int):
         return stream or None
     return stream.cuda_stream or None

@@ -155,6 +155,77 @@ def test_special_values(bits):
         assert same_floats(s, d.host(), s.stepped(h)), eps
 
 
+def _quotients(m, v, h):
+    """A step that leaves m and v as they are and takes m / (sqrt(v) / sqrt(bias2) + eps) * (lr / bias1) off masters
+    of 0: (the kernel's masters, numpy's)."""
+    n = m.size
+    s = R.State([n], 32, F.FR_BF16)
+    s.put(0, "master", np.zeros(n, np.float32))
+    s.put(0, "m", m)
+    s.put(0, "v", v)
+    s.set_grad(0, np.zeros(n, np.float32))
+    d = Dev(s)
+    d.opt.step(d.state, d.grads, hyper_dev(h))
+    got = d.host()
+    assert np.array_equal(s.get(0, "m", got).view(np.uint32), m.view(np.uint32))
+    with np.errstate(all="ignore"):
+        one = np.float32(1)
+        q = m / (np.sqrt(v) * (one / np.sqrt(h[0]["bias2"])) + h[0]["eps"]) * (h[0]["lr"] / h[0]["bias1"])
+        want = np.zeros(n, np.float32) - q
+    return s.get(0, "master", got), want
+
+
+def _same(got, want):
+    return bool(np.all((got.view(np.uint32) == want.view(np.uint32)) | (np.isnan(got) & np.isnan(want))))
+
+
+@pytest.mark.parametrize("case", ["ordinary", "wide", "edges", "one odd value a wave"])
+def test_roots_and_quotients_are_correctly_rounded(case):
+    """4 million quotients of random mantissas against numpy's: operands well inside the range (which take the short
+    form), over all of it (the general form), next to the ends of the short form's ranges, and one element in a wave
+    outside them."""
+    rng = np.random.default_rng(17)
+    n = 1 << 22
+    man = lambda: rng.integers(0, 1 << 23, n).astype(np.uint32)  # noqa: E731
+    lo, hi = {"ordinary": (-40, 20), "wide": (-126, 127), "edges": (-2, 2), "one odd value a wave": (-40, 20)}[case]
+    em, ev = rng.integers(lo, hi, n), rng.integers(lo, hi, n)
+    if case == "edges":
+        em, ev = em + rng.choice([-80, 60, 0], n), ev + rng.choice([-96, 60, 0], n)
+    m = ((em + 127).astype(np.uint32) << 23 | man()).view(np.float32) * rng.choice([-1, 1], n).astype(np.float32)
+    v = ((ev + 127).astype(np.uint32) << 23 | man()).view(np.float32)
+    if case == "one odd value a wave":
+        at = np.arange(0, n, 256) + rng.integers(0, 256, n // 256)
+        m[at[::3]], v[at[1::3]], v[at[2::3]] = 0.0, 0.0, np.float32(1e-42)
+    for bias2, eps in ((1.0, 0.0), (0.25, 1e-8), (1e-9, 1.0), (1.0, 1e13)):
+        h = F.adamw_hyper([dict(lr=1.0, betas=(1.0, 1.0), eps=eps)], 1)
+        h["bias1"], h["bias2"] = 1.0, bias2
+        got, want = _quotients(m, v, h)
+        assert _same(got, want), (bias2, eps)
+
+
+@pytest.mark.parametrize("case", ["ordinary", "wide", "one odd value a wave"])
+def test_roots_of_a_conversion_are_correctly_rounded(case):
+    """Second moments with random mantissas to 8 bits: the codes of the model's correctly rounded roots."""
+    rng = np.random.default_rng(18)
+    n = 1 << 20
+    lo, hi = (-126, 127) if case == "wide" else (-30, 2)
+    v = ((rng.integers(lo, hi, n) + 127).astype(np.uint32) << 23 | rng.integers(0, 1 << 23, n).astype(np.uint32)).view(np.float32)
+    # squares of the borders between codes, and their neighbours, where a root's last place decides
+    c = rng.integers(0, 256, n).astype(np.uint32)
+    border = ((c << 19) + (1 << 18)).astype(np.uint32).view(np.float32) * np.float32(2.0 ** 112)
+    sq = (border.astype(np.float64) ** 2).astype(np.float32).view(np.uint32) + rng.integers(-1, 2, n).astype(np.uint32)
+    pick = rng.random(n) < 0.5
+    v = np.where(pick & (case != "wide"), sq.view(np.float32), v)
+    if case == "one odd value a wave":
+        v[np.arange(0, n, 256) + rng.integers(0, 256, n // 256)] = rng.choice(np.array([0.0, -0.0, 1e-44, 3e-39], np.float32), n // 256)
+    a, b = R.State([n], 32, seed=1), R.State([n], 8, seed=2)
+    a.put(0, "v", v)
+    x, y = Dev(a), Dev(b)
+    for seed in (0, 9):
+        x.opt.convert(x.state, y.opt, y.state, seed)
+        assert first_difference(b, y.host(), a.converted(b, seed)) is None
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 @pytest.mark.parametrize("bad", [np.nan, np.inf])
 def test_a_gradient_that_is_not_finite_stops_the_step(bits, bad):
