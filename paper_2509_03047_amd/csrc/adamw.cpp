@@ -211,6 +211,8 @@ int build(fr_adamw* o) {
                             uint32_t(std::min(t, tiles - i * t)), j});
     }
   }
+  // (a summing step of the same tiles walks the step's table)
+  auto shares_step = [&](int w) { return (w == kSum || w == kSum + 1) && runs[w].tile == runs[w - 2].tile; };
   Carver c;
   const size_t recs = c.add(Y.recs.data(), n * sizeof(AdamwRec));
   const fr_grad_stats neutral = {0.0, 0.0f, 1.0f, 0};
@@ -221,12 +223,13 @@ int build(fr_adamw* o) {
   for (int w = 0; w < kWalks; w++) {
     fi[w] = c.add(runs[w].first.data(), runs[w].first.size() * 8);
     ba[w] = c.add(runs[w].base.data(), runs[w].base.size() * 8);
-    sl[w] = c.add(nullptr, 8 * runs[w].stride() * 8);
+    sl[w] = c.add(nullptr, shares_step(w) ? 0 : 8 * runs[w].stride() * 8);
   }
   for (int f = 0; f < 2; f++) {
     pt[f] = c.add(nullptr, 8 * runs[kSum + f].stride() * (f ? kKinds : kKinds32) * sizeof(fr_chunk_sum));
     fo[f] = c.add(folds[f].data(), folds[f].size() * sizeof(AdamwFold));
   }
+  o->layout.info.device_bytes = c.total;
   hipError_t e = hipMalloc(&o->mem, c.total);
   if (e != hipSuccess) {
     o->mem = nullptr;
@@ -246,6 +249,10 @@ int build(fr_adamw* o) {
   AdamwWalk* walks[kWalks] = {&o->norm, &o->form[0].step, &o->form[1].step, &o->form[0].sum, &o->form[1].sum,
                               &o->form[0].convert, &o->form[1].convert};
   for (int w = 0; w < kWalks; w++) {
+    if (shares_step(w)) {
+      *walks[w] = *walks[w - 2];
+      continue;
+    }
     uint64_t* d = reinterpret_cast<uint64_t*>(at(sl[w]));
     *walks[w] = AdamwWalk{d, runs[w].n(), runs[w].stride()};
     if (e == hipSuccess && runs[w].n())

@@ -80,23 +80,32 @@ struct AdamwConvertArgs {
 
 // How a kernel takes its work: workgroups of B threads with U groups of four
 // elements each, and the LDS a launch asks for to bound how many of them a
-// compute unit holds (adamw.hip says why).
+// compute unit (160 KB) holds; adamw.hip says why, and what a step's measured.
 struct AdamwShape {
   uint32_t B, U, lds;
   constexpr uint32_t tile() const { return B * U * 4; }
 };
-constexpr AdamwShape kStepShape[2] = {{64, 1, 14800}, {64, 2, 6800}};  // by form: 32 bits, 8 bits
-constexpr AdamwShape kSumShape[2] = {{64, 1, 10200}, {64, 1, 0}};   // steps that also sum
-constexpr AdamwShape kConvertShape[2] = {{64, 8, 32000}, {128, 2, 13500}};   // by the form written
-constexpr uint32_t kNormBytes = 16384;  // of gradients a workgroup of a norm takes
-// A norm of more workgroups than this adds up their sums by a second launch of
-// kNormFold; they, or those of a smaller norm, arrive at lines of kNormPerLine
-// each, whose last ones arrive at line 0.
-// (up to kNormOneLine at line 0 themselves: arrivals at one line take 7 ns each,
-// another line a round trip).
+// Times are of an 8B model's share, 1.0e9 elements.
+// By form, 32 bits and 8: 11 and 24 waves a compute unit.  (8 bits: U = 1, no
+// bound 2.78-2.81 ms; U = 2, 20 waves 2.78, 24 waves 2.68-2.70; U = 4, 16 waves 2.70-2.73.)
+constexpr AdamwShape kStepShape[2] = {{64, 1, 14800}, {64, 2, 6800}};
+// Steps that also sum: one wave, which folds its own sums.  (32 bits: 12 waves 4.97-5.04
+// ms, 14 4.79-4.87, 16 4.49-4.53, 20 4.50-4.54; U = 2, 8 waves 4.80, 12 4.53-4.66.  8 bits: U = 1
+// 4.16, U = 2 3.23, U = 4 3.34, where the step and a checksum of the state take 3.8.)
+constexpr AdamwShape kSumShape[2] = {{64, 1, 10200}, {64, 2, 6800}};
+// By the form written: 12 workgroups of two waves and 1,024 elements.  (To 8 bits:
+// 64 x 2, 24 a compute unit 1.63-1.64 ms, 128 x 2, 12 1.62.  To 32: 64 x 2, 24 1.63-1.70,
+// 128 x 2, 12 1.63-1.71, 64 x 8, 5 1.60-1.65, but of 2,000 ragged tensors 69 us where the
+// smaller tiles take 61.)
+constexpr AdamwShape kConvertShape[2] = {{128, 2, 13500}, {128, 2, 13500}};
+constexpr uint32_t kNormBytes = 16384;  // of gradients a workgroup of a norm takes (8 KiB: 374 us instead of 304)
+// A norm of more workgroups than kNormOne adds up their sums by a second launch
+// of kNormFold workgroups; these, or those of a smaller norm, arrive at lines of
+// kNormPerLine each, whose last ones arrive at line 0 (up to kNormOneLine at line
+// 0 themselves: arrivals at one line take 7 ns each, another line a round trip).
 constexpr uint32_t kNormOne = 1024, kNormFold = 64, kNormPerLine = 32, kNormOneLine = 64, kNormLine = 128;
 constexpr uint32_t kNormArriveBytes = (1 + kNormOne / kNormPerLine) * kNormLine;
-static_assert(kSumShape[0].B == 64 && kSumShape[1].B == 64, "one wave, which folds its own sums");
+static_assert(kSumShape[0].B == 64 && kSumShape[1].B == 64, "one wave");
 static_assert(kSumShape[0].tile() * 4 <= FR_ADAMW_MIN_SUM_CHUNK && kSumShape[1].tile() * 4 <= FR_ADAMW_MIN_SUM_CHUNK,
               "a summed tile lies inside a chunk");
 

@@ -3,10 +3,37 @@
 // wrote; the norm of the gradients; moments from one form to the other.
 //
 // All of them stream: an element's state is read and written once (28 bytes
-// with bf16 gradients, 16 with 8-bit moments) for some 20 to 60 instructions,
-// so HBM bounds them.  As in the restore's kernels a workgroup takes one tile,
-// workgroups follow each other in address order, and a slot table says which
-// tile of which tensor each takes.
+// with bf16 gradients, 16 with 8-bit moments) for some 40 to 70 instructions, so
+// HBM bounds them, at the 6.4-6.6 TB/s that a copy reaches (reads alone: 7.1);
+// the 8-bit step comes near the vector units' bound as well (below).  A slot
+// table says which tile of which tensor each workgroup takes, in address order,
+// as in the restore's kernels.  What decides beyond that:
+//
+//   * The window.  A step reads three or four arrays and writes four, so the
+//     memory that all workgroups touch at one time is seven windows, each as
+//     wide as the tiles in flight.  With 8 workgroups of 256 threads and 2,048
+//     elements on each compute unit the step of an 8B model's share (1.0e9
+//     elements, bf16 gradients) ran at 6.3 TB/s in some allocations and 5.5 in
+//     most, for hours, whatever the arrays' offsets to each other; the smaller
+//     the windows, the smaller the gap.  One wave and 256 elements a workgroup
+//     and 11 workgroups a compute unit close it: 4.29 ms, 6.55 TB/s, in all (10:
+//     4.32; 13: 4.34; 16: 4.45-4.51; 128 threads, 6 a compute unit: 4.33-4.51;
+//     256 threads, 3: 4.67-4.82).  The number is set by LDS that the launch asks
+//     for and nothing uses, as there is no other limit short of the registers'.
+//     With less work in flight the chain of dependent loads (slot, record,
+//     hyperparameters, data) is what a tile waits for, so everything that does
+//     not depend on the data is loaded before it, and computed behind it.
+//     The other kernels have more instructions or fewer bytes a tile, which
+//     takes more of them; their numbers (adamw.h) are the best of similar sweeps.
+//   * Instructions, in 8 bits: hardware conversions from fp8 and to bf16, short
+//     forms of root and quotient where the operands allow them, one scale a
+//     wave (so that it is a scalar), codes rounded in place in the top bytes of
+//     the words they are packed from: 83 -> 67 instructions an element, 2.92 ->
+//     2.68 ms, 6.0 TB/s.  The vector units are then busy for two thirds of it.
+//   * Sums are folded by the wave that made them (wave_totals) and left 64 or 96
+//     bytes a tile for a second kernel: a step with them takes 4.50 ms, where the
+//     step and a checksum of the state take 6.3.
+//   * No release and acquire between workgroups (finish_norm).
 //
 // The arithmetic is that of the header, operation by operation: no contraction
 // to fused multiply-adds, sqrt and divisions correctly rounded.
@@ -51,27 +78,37 @@ __device__ __forceinline__ Tile tile_of(const AdamwWalk& w, const AdamwRec* recs
   return t;
 }
 
-// Elements i ... i + 3 of the n at p, zeros behind them; kFull: all four are there.
+// Elements i ... i + 3 of the n > 0 at p, zeros behind them; kFull: all four are
+// there.  Else each comes by a load of its own, from the last one's place where
+// there is none: without branches all loads are in flight together.  (A load
+// within a branch is waited for before the branch ends: a step of 20,000
+// tensors of 1 to 4,096 elements took 81 us instead of 62.)
 template <bool kFull>
 __device__ __forceinline__ u32x4 load4(const void* p, uint32_t i, uint32_t n) {
-  const uint32_t* q = static_cast<const uint32_t*>(p) + i;
-  if (kFull || i + 4 <= n) return ld_nt(reinterpret_cast<const u32x4*>(q));
-  u32x4 x = {0, 0, 0, 0};
-  for (int j = 0; j < 4; j++)
-    if (i + j < n) x[j] = q[j];
+  const uint32_t* q = static_cast<const uint32_t*>(p);
+  if constexpr (kFull) return ld_nt(reinterpret_cast<const u32x4*>(q + i));
+  u32x4 x;
+#pragma unroll
+  for (uint32_t j = 0; j < 4; j++) x[j] = q[i + j < n ? i + j : n - 1];
+#pragma unroll
+  for (uint32_t j = 0; j < 4; j++) x[j] = i + j < n ? x[j] : 0u;
   return x;
 }
 // The same of bf16 elements, in the first two words.
 template <bool kFull>
 __device__ __forceinline__ u32x4 load4h(const void* p, uint32_t i, uint32_t n) {
-  const uint16_t* q = static_cast<const uint16_t*>(p) + i;
+  const uint16_t* q = static_cast<const uint16_t*>(p);
   u32x4 x = {0, 0, 0, 0};
-  if (kFull || i + 4 <= n) {
-    x.xy = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(q));
+  if constexpr (kFull) {
+    x.xy = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(q + i));
     return x;
   }
-  for (int j = 0; j < 4; j++)
-    if (i + j < n) x[j / 2] |= uint32_t(q[j]) << (16 * (j & 1));
+  uint32_t h[4];
+#pragma unroll
+  for (uint32_t j = 0; j < 4; j++) h[j] = q[i + j < n ? i + j : n - 1];
+#pragma unroll
+  for (uint32_t j = 0; j < 4; j++) h[j] = i + j < n ? h[j] : 0u;
+  x.xy = u32x2{h[0] | h[1] << 16, h[2] | h[3] << 16};
   return x;
 }
 // Their fp32 patterns.
@@ -102,6 +139,22 @@ __device__ __forceinline__ uint32_t load_codes(const uint8_t* p) {
 }
 __device__ __forceinline__ void store_codes(uint32_t c, uint8_t* p) {
   __builtin_nontemporal_store(c, reinterpret_cast<uint32_t*>(p));
+}
+
+// Codes of elements i ... i + 3 and their block's scales (zeros behind the n > 0
+// elements, by loads from the last place as in load4).
+template <bool kFull>
+__device__ __forceinline__ void load_block(const uint8_t* pm, const uint8_t* pv, const float* psm, const float* psv,
+                                           uint32_t i, uint32_t n, uint32_t* cm, uint32_t* cv, float* sm, float* sv) {
+  const uint32_t at = kFull || i < n ? i : (n - 1) & ~3u, b = at / FR_ADAMW_BLOCK;
+  *cm = load_codes(pm + at);
+  *cv = load_codes(pv + at);
+  *sm = psm[b];
+  *sv = psv[b];
+  if (!kFull && i >= n) {
+    *cm = *cv = 0;
+    *sm = *sv = 0.0f;
+  }
 }
 
 // The largest of a wave's 64 values, in all lanes (a scalar): four steps within
@@ -375,15 +428,10 @@ __device__ __forceinline__ void step_tile(const StepCtx& t, u64 (&s)[K], u64 (&w
   float sm[U] = {}, sv[U] = {};
 #pragma unroll
   for (int q = 0; q < U; q++) {
-    const uint32_t i = (q * B + threadIdx.x) * 4, b = i / FR_ADAMW_BLOCK;  // the wave's block
+    const uint32_t i = (q * B + threadIdx.x) * 4;
     uw[q] = load4<kFull>(t.pw, i, n);
     if constexpr (kEight) {
-      if (kFull || i < n) {
-        cm[q] = load_codes(t.pm + i);
-        cv[q] = load_codes(t.pv + i);
-        sm[q] = t.psm[b];
-        sv[q] = t.psv[b];
-      }
+      load_block<kFull>(t.pm, t.pv, t.psm, t.psv, i, n, &cm[q], &cv[q], &sm[q], &sv[q]);
     } else {
       um[q] = load4<kFull>(t.pm, i, n);
       uv[q] = load4<kFull>(t.pv, i, n);
@@ -394,7 +442,7 @@ __device__ __forceinline__ void step_tile(const StepCtx& t, u64 (&s)[K], u64 (&w
   if (k.skip && !kSums) return;
 #pragma unroll
   for (int q = 0; q < U; q++) {
-    const uint32_t i = (q * B + threadIdx.x) * 4, b = i / FR_ADAMW_BLOCK;
+    const uint32_t i = (q * B + threadIdx.x) * 4, b = i / FR_ADAMW_BLOCK;  // the wave's block
     f32x4 m, v;
     u32x2 up = {0, 0};
     if constexpr (kEight) {
@@ -706,14 +754,9 @@ __device__ __forceinline__ void convert_tile(const ConvertCtx& t) {
   float sm[U] = {}, sv[U] = {};
 #pragma unroll
   for (int q = 0; q < U; q++) {
-    const uint32_t i = (q * B + threadIdx.x) * 4, b = i / FR_ADAMW_BLOCK;
+    const uint32_t i = (q * B + threadIdx.x) * 4;
     if constexpr (k8From) {
-      if (kFull || i < n) {
-        cm[q] = load_codes(t.qm + i);
-        cv[q] = load_codes(t.qv + i);
-        sm[q] = t.qsm[b];
-        sv[q] = t.qsv[b];
-      }
+      load_block<kFull>(t.qm, t.qv, t.qsm, t.qsv, i, n, &cm[q], &cv[q], &sm[q], &sv[q]);
     } else {
       um[q] = load4<kFull>(t.qm, i, n);
       uv[q] = load4<kFull>(t.qv, i, n);

@@ -81,7 +81,8 @@ class fr_plan_info(C.Structure):
 
 class fr_adamw_info(C.Structure):
     _fields_ = [(f, C.c_uint64) for f in ("n_tensors", "n_groups", "n_elements", "n_elements_8bit", "n_counters",
-                                          "grad_arena_bytes", "arena_bytes", "sums_chunks")] + [("device", C.c_int64)]
+                                          "grad_arena_bytes", "arena_bytes", "sums_chunks",
+                                          "device_bytes")] + [("device", C.c_int64)]
 
     def as_dict(self):
         return {f: getattr(self, f) for f, _ in self._fields_}

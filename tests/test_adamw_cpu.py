@@ -207,3 +207,28 @@ def test_step_in_32_bits_is_the_step_in_64():
     assert np.all(np.abs(m32 - m64) <= 5 * u * am)
     assert np.all(np.abs(v32 - v64) <= 7 * u * v64)
     assert np.all(np.abs(w32 - w64) <= 4 * u * aw + 20 * u * au)
+
+
+@pytest.mark.slow
+def test_host_code_under_sanitizers(tmp_path):
+    """tests/host/adamw_fuzz.cpp with the optimizer's and the plan's host code, the kernel launchers (never reached)
+    left out."""
+    import os
+    import shutil
+    import subprocess
+
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    csrc, rocm = os.path.join(root, "paper_2509_03047_amd", "csrc"), os.environ.get("ROCM_PATH", "/opt/rocm")
+    if shutil.which("g++") is None or not os.path.isdir(os.path.join(rocm, "include", "hip")):
+        pytest.skip("needs g++ and the HIP headers")
+    exe = str(tmp_path / "adamw_fuzz")
+    b = subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
+                        "-D__HIP_PLATFORM_AMD__", "-I", os.path.join(root, "include"), "-I", csrc,
+                        "-I", os.path.join(rocm, "include"), os.path.join(root, "tests", "host", "adamw_fuzz.cpp"),
+                        os.path.join(csrc, "adamw.cpp"), os.path.join(csrc, "plan.cpp"),
+                        "-L", os.path.join(rocm, "lib"), "-lamdhip64", "-Wl,-rpath," + os.path.join(rocm, "lib"),
+                        "-Wl,--unresolved-symbols=ignore-all", "-o", exe], capture_output=True, text=True, timeout=600)
+    assert b.returncode == 0, b.stderr[-3000:]
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=600)
+    assert r.returncode == 0, (r.stdout + r.stderr)[-3000:]
+    assert " 0 wrong" in r.stdout
