@@ -152,7 +152,8 @@ struct fr_adamw {
     AdamwWalk step, sum, convert;
     fr_chunk_sum* parts = nullptr;
     const AdamwFold* folds = nullptr;
-    uint32_t n_folds = 0;
+    const AdamwScales* scales = nullptr;
+    uint32_t n_folds = 0, n_scales = 0;
   } form[2];
   const fr_grad_stats* no_stats = nullptr;  // scale 1: a step without statistics reads these
   AdamwWalk norm;
@@ -187,6 +188,7 @@ int build(fr_adamw* o) {
                        Runs(kSumShape[0].tile()), Runs(kSumShape[1].tile()),
                        Runs(kConvertShape[0].tile()), Runs(kConvertShape[1].tile())};
   std::vector<AdamwFold> folds[2];
+  std::vector<AdamwScales> scales[2];
   const bool sums = o->C >= FR_ADAMW_MIN_SUM_CHUNK;
   for (uint32_t k = 0; k < n; k++) {
     const uint32_t f = Y.eight[k];
@@ -201,14 +203,19 @@ int build(fr_adamw* o) {
     w.add(k, numel);
     const uint64_t tiles = w.n() - first;
     // chunk i of an array holds this many elements, and so these tiles
-    const uint64_t per[kKinds] = {o->C / 2, o->C / 4, f ? o->C : o->C / 4, f ? o->C : o->C / 4,
-                                  o->C / 4 * FR_ADAMW_BLOCK, o->C / 4 * FR_ADAMW_BLOCK};
+    const uint64_t per[kSummed] = {o->C / 2, o->C / 4, f ? o->C : o->C / 4, f ? o->C : o->C / 4};
     for (uint32_t j = 0; j < kKinds; j++) {
       if (Y.recs[k].at[j] == kNone) continue;
-      const uint64_t t = per[j] / w.tile;
-      for (uint64_t i = 0; i < Y.n_chunks[size_t(k) * kKinds + j]; i++)
-        folds[f].push_back({Y.chunk0[size_t(k) * kKinds + j] + uint32_t(i), uint32_t(first + i * t),
-                            uint32_t(std::min(t, tiles - i * t)), j});
+      const uint32_t chunk0 = Y.chunk0[size_t(k) * kKinds + j], n_chunks = Y.n_chunks[size_t(k) * kKinds + j];
+      for (uint32_t i = 0; i < n_chunks; i++) {
+        if (j < kSummed) {
+          const uint64_t t = per[j] / w.tile;
+          folds[f].push_back({chunk0 + i, uint32_t(first + i * t), uint32_t(std::min(t, tiles - i * t)), j});
+        } else {
+          const uint64_t words = o->C / 4, from = i * words;
+          scales[f].push_back({Y.recs[k].at[j] + i * o->C, uint32_t(std::min(words, blocks_of(numel) - from)), chunk0 + i});
+        }
+      }
     }
   }
   // (a summing step of the same tiles walks the step's table)
@@ -219,15 +226,16 @@ int build(fr_adamw* o) {
   const size_t ns = c.add(&neutral, sizeof neutral);
   const size_t np = c.add(nullptr, (8 * runs[kNorm].stride() + kNormFold) * sizeof(double));
   const size_t ar = c.add(nullptr, kNormArriveBytes);
-  size_t fi[kWalks], ba[kWalks], sl[kWalks], pt[2], fo[2];
+  size_t fi[kWalks], ba[kWalks], sl[kWalks], pt[2], fo[2], sc[2];
   for (int w = 0; w < kWalks; w++) {
     fi[w] = c.add(runs[w].first.data(), runs[w].first.size() * 8);
     ba[w] = c.add(runs[w].base.data(), runs[w].base.size() * 8);
     sl[w] = c.add(nullptr, shares_step(w) ? 0 : 8 * runs[w].stride() * 8);
   }
   for (int f = 0; f < 2; f++) {
-    pt[f] = c.add(nullptr, 8 * runs[kSum + f].stride() * (f ? kKinds : kKinds32) * sizeof(fr_chunk_sum));
+    pt[f] = c.add(nullptr, 8 * runs[kSum + f].stride() * kSummed * sizeof(fr_chunk_sum));
     fo[f] = c.add(folds[f].data(), folds[f].size() * sizeof(AdamwFold));
+    sc[f] = c.add(scales[f].data(), scales[f].size() * sizeof(AdamwScales));
   }
   o->layout.info.device_bytes = c.total;
   hipError_t e = hipMalloc(&o->mem, c.total);
@@ -270,7 +278,9 @@ int build(fr_adamw* o) {
   for (int f = 0; f < 2; f++) {
     o->form[f].parts = reinterpret_cast<fr_chunk_sum*>(at(pt[f]));
     o->form[f].folds = reinterpret_cast<const AdamwFold*>(at(fo[f]));
+    o->form[f].scales = reinterpret_cast<const AdamwScales*>(at(sc[f]));
     o->form[f].n_folds = uint32_t(folds[f].size());
+    o->form[f].n_scales = uint32_t(scales[f].size());
   }
   return FR_OK;
 }
@@ -453,7 +463,9 @@ extern "C" int fr_adamw_step(const fr_adamw* opt, void* state, const void* grads
       a.C = opt->C;
       a.parts = F.parts;
       a.folds = F.folds;
+      a.scales = F.scales;
       a.n_folds = F.n_folds;
+      a.n_scales = F.n_scales;
       a.sums = sums;
     }
     FR_TRY(launch_result(launch_adamw_step(a, stream)));

@@ -9,9 +9,9 @@
 
 namespace fr {
 
-// The arrays of a tensor whose chunks a step can sum, in this order.
+// The arrays of a tensor.
 enum AdamwKind : uint32_t { kParam, kMaster, kMom1, kMom2, kScale1, kScale2, kKinds };
-constexpr uint32_t kKinds32 = kMom2 + 1;  // those of a tensor with 32-bit moments
+constexpr uint32_t kSummed = kMom2 + 1;  // the first ones, which a step sums as it writes them
 
 // One tensor, as the kernels read it (uniform loads).  Offsets from the state
 // arena's base, `grad` from the gradients'.
@@ -40,6 +40,13 @@ struct AdamwWalk {
 struct alignas(16) AdamwFold {
   uint32_t chunk, slot, n, kind;
 };
+// A chunk of scales, which is summed from the state itself once the step has
+// written it: a wave's two scales would take as much to leave and fold as their
+// whole chunk to read, and a chunk of C bytes is fed by C / 8 waves.
+struct alignas(16) AdamwScales {
+  uint64_t at;  // in the state
+  uint32_t words, chunk;
+};
 
 // What the kernels of one call need of its optimizer.
 struct AdamwStepArgs {
@@ -52,9 +59,10 @@ struct AdamwStepArgs {
   const fr_grad_stats* stats = nullptr;
   // sums, or parts == NULL
   uint64_t C = 0;
-  fr_chunk_sum* parts = nullptr;  // walk.stride * 8 places of kKinds32 or kKinds sums
+  fr_chunk_sum* parts = nullptr;  // kSummed arrays of 8 * walk.stride places
   const AdamwFold* folds = nullptr;
-  uint32_t n_folds = 0;
+  const AdamwScales* scales = nullptr;
+  uint32_t n_folds = 0, n_scales = 0;
   fr_chunk_sum* sums = nullptr;
 };
 
@@ -89,10 +97,11 @@ struct AdamwShape {
 // By form, 32 bits and 8: 11 and 24 waves a compute unit.  (8 bits: U = 1, no
 // bound 2.78-2.81 ms; U = 2, 20 waves 2.78, 24 waves 2.68-2.70; U = 4, 16 waves 2.70-2.73.)
 constexpr AdamwShape kStepShape[2] = {{64, 1, 14800}, {64, 2, 6800}};
-// Steps that also sum: one wave, which folds its own sums.  (32 bits: 12 waves 4.97-5.04
-// ms, 14 4.79-4.87, 16 4.49-4.53, 20 4.50-4.54; U = 2, 8 waves 4.80, 12 4.53-4.66.  8 bits: U = 1
-// 4.16, U = 2 3.23, U = 4 3.34, where the step and a checksum of the state take 3.8.)
-constexpr AdamwShape kSumShape[2] = {{64, 1, 10200}, {64, 2, 6800}};
+// Steps that also sum: one wave, which folds its own sums; 16 and 32 waves.  (32
+// bits: 12 waves 4.97-5.04 ms, 14 4.79-4.87, 16 4.49-4.53, 20 4.50-4.54; U = 2, 8 waves 4.80,
+// 12 4.53-4.66.  8 bits: U = 1 3.03-3.19; U = 2, 16 waves 3.20-3.34, 24 2.96-3.06, no bound
+// 2.84-3.00, where the step and a checksum of the state take 3.8.)
+constexpr AdamwShape kSumShape[2] = {{64, 1, 10200}, {64, 2, 0}};
 // By the form written: 12 workgroups of two waves and 1,024 elements.  (To 8 bits:
 // 64 x 2, 24 a compute unit 1.63-1.64 ms, 128 x 2, 12 1.62.  To 32: 64 x 2, 24 1.63-1.70,
 // 128 x 2, 12 1.63-1.71, 64 x 8, 5 1.60-1.65, but of 2,000 ragged tensors 69 us where the

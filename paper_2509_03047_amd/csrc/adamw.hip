@@ -30,9 +30,9 @@
 //     wave (so that it is a scalar), codes rounded in place in the top bytes of
 //     the words they are packed from: 83 -> 67 instructions an element, 2.92 ->
 //     2.68 ms, 6.0 TB/s.  The vector units are then busy for two thirds of it.
-//   * Sums are folded by the wave that made them (wave_totals) and left 64 or 96
-//     bytes a tile for a second kernel: a step with them takes 4.50 ms, where the
-//     step and a checksum of the state take 6.3.
+//   * Sums are folded by the wave that made them (wave_totals) and left 64 bytes
+//     a tile for a second kernel: a step with them takes 4.53 ms, where the step
+//     and a checksum of the state take 6.3 (8 bits: 2.90 and 3.8).
 //   * No release and acquire between workgroups (finish_norm).
 //
 // The arithmetic is that of the header, operation by operation: no contraction
@@ -329,19 +329,18 @@ __device__ __forceinline__ f32x4 roots(const f32x4& v) {
 
 // --------------------------------------------------------------------- step
 
-// Sums over a wave of N (8 or 16) 64-bit values at once.  Each of the first
-// steps brings the lanes together in pairs that keep one half of the values
-// each, so that N values take N - 1 exchanges and the last steps for one value
-// instead of 6 N: with 8 values a quarter of the instructions.  Lane l ends with
-// the total of value l / (64 / N).
+// Sums over a wave of eight 64-bit values at once.  Each of the first steps
+// brings the lanes together in pairs that keep one half of the values each, so
+// that they take 4 + 2 + 1 exchanges and the last three steps are of one value:
+// 10 exchanges instead of 48.  Lane l ends with the total of value l / 8.
 template <int kCtrl>
 __device__ __forceinline__ u64 dpp64(u64 x) {
   const uint32_t lo = __builtin_amdgcn_update_dpp(0u, uint32_t(x), kCtrl, 0xF, 0xF, true);
   const uint32_t hi = __builtin_amdgcn_update_dpp(0u, uint32_t(x >> 32), kCtrl, 0xF, 0xF, true);
   return u64(hi) << 32 | lo;
 }
-// a + b, where lanes whose bit 5 (32) or 4 (16) is set keep b's sums and the
-// others a's.
+// The sums of a with the lanes 32 (or 16) apart in the lanes whose bit 5 (4) is
+// clear, those of b in the others.
 template <int kLanes>
 __device__ __forceinline__ u64 halve(u64 a, u64 b) {
   const uint32_t al = uint32_t(a), ah = uint32_t(a >> 32), bl = uint32_t(b), bh = uint32_t(b >> 32);
@@ -355,27 +354,17 @@ __device__ __forceinline__ u64 halve(u64 a, u64 b) {
     return (u64(hi[0]) << 32 | lo[0]) + (u64(hi[1]) << 32 | lo[1]);
   }
 }
-// The same for bit 3 (row_ror:8) or 2 (row_half_mirror) of the lane.
-template <int kLanes>
-__device__ __forceinline__ u64 halve_dpp(u64 a, u64 b) {
-  const bool upper = threadIdx.x & kLanes;
-  const u64 keep = upper ? b : a, send = upper ? a : b;
-  return keep + dpp64 < kLanes == 8 ? 0x128 : 0x141 > (send);
-}
-template <int N>
-__device__ __forceinline__ u64 wave_totals(u64 (&x)[N]) {
-  static_assert(N == 8 || N == 16, "");
+__device__ __forceinline__ u64 wave_totals(u64 (&x)[8]) {
 #pragma unroll
-  for (int i = 0; i < N / 2; i++) x[i] = halve<32>(x[i], x[i + N / 2]);
+  for (int i = 0; i < 4; i++) x[i] = halve<32>(x[i], x[i + 4]);
 #pragma unroll
-  for (int i = 0; i < N / 4; i++) x[i] = halve<16>(x[i], x[i + N / 4]);
-#pragma unroll
-  for (int i = 0; i < N / 8; i++) x[i] = halve_dpp<8>(x[i], x[i + N / 8]);
-  u64 t = x[0];
-  if constexpr (N == 16) t = halve_dpp<4>(x[0], x[1]);
-  else t += dpp64<0x141>(t);  // row_half_mirror
-  t += dpp64<0x4E>(t);        // quad_perm: lanes 2 apart
-  return t + dpp64<0xB1>(t);  // and neighbours
+  for (int i = 0; i < 2; i++) x[i] = halve<16>(x[i], x[i + 2]);
+  const bool upper = threadIdx.x & 8;
+  const u64 keep = upper ? x[1] : x[0], send = upper ? x[0] : x[1];
+  u64 t = keep + dpp64<0x128>(send);  // row_ror:8
+  t += dpp64<0x141>(t);               // row_half_mirror
+  t += dpp64<0x4E>(t);                // quad_perm: lanes 2 apart
+  return t + dpp64<0xB1>(t);          // and neighbours
 }
 
 // A value that is the same in all of a wave's lanes that hold one (lane 0 does).
@@ -390,7 +379,7 @@ struct StepCtx {
   uint64_t counter;
   fr_adamw_hyper hyper;  // its group's
   fr_grad_stats stats;
-  uint32_t word4, word2, word1, wordb;  // first word of the tile in its chunks, by bytes an element (b: of scales)
+  uint32_t word4, word2, word1;  // first word of the tile in its chunks, by bytes an element
 };
 
 // The constants of a step, each with the header's roundings.
@@ -420,8 +409,8 @@ __device__ __forceinline__ StepConsts consts_of(const fr_adamw_hyper& h, const f
 // One tile.  kFull: it is whole, so that nothing is predicated; kGrad32: fp32
 // gradients.  All loads are issued before anything is waited for, the
 // constants among it.
-template <bool kEight, bool kSums, bool kFull, bool kGrad32, int B, int U, int K>
-__device__ __forceinline__ void step_tile(const StepCtx& t, u64 (&s)[K], u64 (&ws)[K]) {
+template <bool kEight, bool kSums, bool kFull, bool kGrad32, int B, int U>
+__device__ __forceinline__ void step_tile(const StepCtx& t, u64 (&s)[kSummed], u64 (&ws)[kSummed]) {
   const uint32_t n = kFull ? B * U * 4 : t.n;
   u32x4 uw[U], um[U], uv[U], ug[U];
   uint32_t cm[U] = {}, cv[U] = {};
@@ -513,13 +502,6 @@ __device__ __forceinline__ void step_tile(const StepCtx& t, u64 (&s)[K], u64 (&w
         ws[kMom1] += i1 * cm[q];
         s[kMom2] += cv[q];
         ws[kMom2] += i1 * cv[q];
-        if ((kFull || i < n) && threadIdx.x % 64 == 0) {
-          const u64 is = t.wordb + b + 1;
-          s[kScale1] += as_u(sm[q]);
-          ws[kScale1] += is * as_u(sm[q]);
-          s[kScale2] += as_u(sv[q]);
-          ws[kScale2] += is * as_u(sv[q]);
-        }
       } else {
         acc4(um[q], t.word4 + i, s[kMom1], ws[kMom1]);
         acc4(uv[q], t.word4 + i, s[kMom2], ws[kMom2]);
@@ -534,7 +516,6 @@ __global__ __launch_bounds__(B) void k_adamw(const AdamwRec* __restrict__ recs, 
                                              const fr_adamw_hyper* __restrict__ hyper,
                                              const fr_grad_stats* __restrict__ stats, uint64_t C,
                                              fr_chunk_sum* __restrict__ parts) {
-  constexpr int K = kEight ? int(kKinds) : int(kKinds32);
   const Tile t = tile_of<B * U * 4>(walk, recs, blockIdx.x);
   StepCtx c;
   c.n = t.n;
@@ -554,10 +535,9 @@ __global__ __launch_bounds__(B) void k_adamw(const AdamwRec* __restrict__ recs, 
     c.word4 = uint32_t(4 * t.e0 & mask) / 4;
     c.word2 = uint32_t(2 * t.e0 & mask) / 4;
     c.word1 = uint32_t(t.e0 & mask) / 4;
-    c.wordb = uint32_t(t.e0 / FR_ADAMW_BLOCK * 4 & mask) / 4;
   }
 
-  u64 s[K] = {}, ws[K] = {};
+  u64 s[kSummed] = {}, ws[kSummed] = {};
   if (t.n == B * U * 4) {
     if (t.r.grad_f32) step_tile<kEight, kSums, true, true, B, U>(c, s, ws);
     else step_tile<kEight, kSums, true, false, B, U>(c, s, ws);
@@ -567,37 +547,69 @@ __global__ __launch_bounds__(B) void k_adamw(const AdamwRec* __restrict__ recs, 
   }
   if constexpr (kSums) {
     static_assert(B == 64, "a wave");
-    constexpr int N = K <= 4 ? 8 : 16;
-    u64 x[N] = {};
+    u64 x[8];
 #pragma unroll
-    for (int k = 0; k < K; k++) {
+    for (int k = 0; k < 4; k++) {
       x[2 * k] = s[k];
       x[2 * k + 1] = ws[k];
     }
     const u64 total = wave_totals(x);
-    const uint32_t v = threadIdx.x / (64 / N);
-    if (threadIdx.x % (64 / N) == 0 && v < 2 * K)
-      reinterpret_cast<u64*>(parts + uint64_t(t.place) * K)[v] = total;
+    const uint32_t v = threadIdx.x / 8;
+    if (threadIdx.x % 8 == 0)
+      reinterpret_cast<u64*>(parts + (uint64_t(v / 2) * 8 * walk.stride + t.place))[v % 2] = total;
   }
 }
 
-// A chunk's sums from what its tiles left: 16 lanes a chunk.
-template <int K>
-__global__ __launch_bounds__(256) void k_adamw_fold(const AdamwFold* folds, uint32_t n_folds, uint64_t stride,
-                                                    const fr_chunk_sum* parts, fr_chunk_sum* sums) {
-  const uint32_t f = (blockIdx.x * 256 + threadIdx.x) / 16, lane = threadIdx.x % 16;
+// The sums of chunks.  The first n_scales workgroups read a chunk of scales
+// each; the others take what the tiles of a chunk left, L lanes a chunk: as many
+// as make the loads of a long chunk one or two in a row.  Places are kept array
+// by array, so that what one chunk needs is contiguous.
+template <int L>
+__global__ __launch_bounds__(256) void k_adamw_fold(const AdamwFold* folds, uint32_t n_folds,
+                                                    const AdamwScales* scales, uint32_t n_scales, uint64_t stride,
+                                                    const fr_chunk_sum* parts, const uint8_t* state,
+                                                    fr_chunk_sum* sums) {
   u64 s = 0, ws = 0;
+  if (blockIdx.x < n_scales) {
+    const AdamwScales d = scales[blockIdx.x];
+    const u32x4* const p = reinterpret_cast<const u32x4*>(state + d.at);
+#pragma unroll 4
+    for (uint32_t i = threadIdx.x; i < d.words / 4; i += 256) acc4(p[i], 4 * i, s, ws);
+    const uint32_t last = d.words / 4 * 4 + threadIdx.x;
+    if (last < d.words) {
+      const uint32_t w = reinterpret_cast<const uint32_t*>(p)[last];
+      s += w;
+      ws += u64(last + 1) * w;
+    }
+    __shared__ u64 part[8];
+#pragma unroll
+    for (int x = 32; x; x >>= 1) {
+      s += __shfl_xor(s, x);
+      ws += __shfl_xor(ws, x);
+    }
+    if (threadIdx.x % 64 == 0) {
+      part[threadIdx.x / 64] = s;
+      part[4 + threadIdx.x / 64] = ws;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0)
+      sums[d.chunk] = fr_chunk_sum{part[0] + part[1] + part[2] + part[3], part[4] + part[5] + part[6] + part[7]};
+    return;
+  }
+  const uint32_t f = ((blockIdx.x - n_scales) * 256 + threadIdx.x) / L, lane = threadIdx.x % L;
   AdamwFold d = {};
   if (f < n_folds) {
     d = folds[f];
-    for (uint32_t j = lane; j < d.n; j += 16) {
+#pragma unroll 2
+    for (uint32_t j = lane; j < d.n; j += L) {
       const uint64_t g = uint64_t(d.slot) + j;
-      const fr_chunk_sum x = parts[((g & 7) * stride + (g >> 3)) * K + d.kind];
+      const fr_chunk_sum x = parts[(d.kind * 8 + (g & 7)) * stride + (g >> 3)];
       s += x.sum;
       ws += x.wsum;
     }
   }
-  for (int x = 8; x; x >>= 1) {
+#pragma unroll
+  for (int x = L / 2; x; x >>= 1) {
     s += __shfl_xor(s, x);
     ws += __shfl_xor(ws, x);
   }
@@ -825,9 +837,15 @@ int step(const AdamwStepArgs& a, hipStream_t st) {
                      a.parts);
   const int e = int(hipGetLastError());
   if (e != 0 || !kSums || a.n_folds == 0) return e;
-  constexpr int K = kEight ? int(kKinds) : int(kKinds32);
-  hipLaunchKernelGGL((k_adamw_fold<K>), dim3((a.n_folds + 15) / 16), dim3(256), 0, st, a.folds, a.n_folds,
-                     a.walk.stride, a.parts, a.sums);
+  // tiles of the longest chunks that are fed by tiles: parameters', or codes'
+  const uint64_t tiles = a.C / (kEight ? 1 : 2) / s.tile();
+  const auto fold = [&](auto kernel, uint32_t lanes) {
+    const uint32_t per = 256 / lanes;
+    hipLaunchKernelGGL(kernel, dim3(a.n_scales + (a.n_folds + per - 1) / per), dim3(256), 0, st, a.folds, a.n_folds,
+                       a.scales, a.n_scales, a.walk.stride, a.parts, static_cast<const uint8_t*>(a.state), a.sums);
+  };
+  if (tiles >= 64) fold(k_adamw_fold<64>, 64);
+  else fold(k_adamw_fold<16>, 16);
   return int(hipGetLastError());
 }
 
