@@ -14,8 +14,8 @@
 //     wide as the tiles in flight.  With 8 workgroups of 256 threads and 2,048
 //     elements on each compute unit the step of an 8B model's share (1.0e9
 //     elements, bf16 gradients) ran at 6.3 TB/s in some allocations and 5.5 in
-//     most, for hours, whatever the arrays' offsets to each other; the smaller
-//     the windows, the smaller the gap.  One wave and 256 elements a workgroup
+//     most, whatever the arrays' offsets to each other; the smaller the windows,
+//     the smaller the gap.  One wave and 256 elements a workgroup
 //     and 11 workgroups a compute unit close it: 4.29 ms, 6.55 TB/s, in all (10:
 //     4.32; 13: 4.34; 16: 4.45-4.51; 128 threads, 6 a compute unit: 4.33-4.51;
 //     256 threads, 3: 4.67-4.82).  The number is set by LDS that the launch asks
@@ -29,7 +29,8 @@
 //     forms of root and quotient where the operands allow them, one scale a
 //     wave (so that it is a scalar), codes rounded in place in the top bytes of
 //     the words they are packed from: 83 -> 67 instructions an element, 2.92 ->
-//     2.68 ms, 6.0 TB/s.  The vector units are then busy for two thirds of it.
+//     2.55-2.73 ms by allocation, 5.9-6.3 TB/s.  The vector units are then busy
+//     for two thirds of it.
 //   * Sums are folded by the wave that made them (wave_totals) and left 64 bytes
 //     a tile for a second kernel: a step with them takes 4.53 ms, where the step
 //     and a checksum of the state take 6.3 (8 bits: 2.90 and 3.8).
@@ -561,10 +562,13 @@ __global__ __launch_bounds__(B) void k_adamw(const AdamwRec* __restrict__ recs, 
 }
 
 // The sums of chunks.  The first n_scales workgroups read a chunk of scales
-// each; the others take what the tiles of a chunk left, L lanes a chunk: as many
-// as make the loads of a long chunk one or two in a row.  Places are kept array
-// by array, so that what one chunk needs is contiguous.
-template <int L>
+// each; the others take what the tiles of a chunk left, L lanes a chunk and four
+// loads of each in flight (past the end the last one again, not counted).  Places
+// are kept array by array, so that what one chunk needs is contiguous.  A wave a
+// chunk costs an 8B model's share in chunks of 64 KiB, 215,000 of them, 97 us
+// where 16 lanes take 59; a chunk of 512 tiles wants the wave (a state of 3.7M
+// elements, chunks of 256 KiB, step and sums: 26.1 us with 16 lanes, 23.6 with 64).
+template <uint32_t L>
 __global__ __launch_bounds__(256) void k_adamw_fold(const AdamwFold* folds, uint32_t n_folds,
                                                     const AdamwScales* scales, uint32_t n_scales, uint64_t stride,
                                                     const fr_chunk_sum* parts, const uint8_t* state,
@@ -600,12 +604,20 @@ __global__ __launch_bounds__(256) void k_adamw_fold(const AdamwFold* folds, uint
   AdamwFold d = {};
   if (f < n_folds) {
     d = folds[f];
-#pragma unroll 2
-    for (uint32_t j = lane; j < d.n; j += L) {
-      const uint64_t g = uint64_t(d.slot) + j;
-      const fr_chunk_sum x = parts[(d.kind * 8 + (g & 7)) * stride + (g >> 3)];
-      s += x.sum;
-      ws += x.wsum;
+    const fr_chunk_sum* const p = parts + uint64_t(d.kind) * 8 * stride;
+    constexpr uint32_t kLoads = 4;
+    for (uint32_t j = lane; j < d.n; j += kLoads * L) {
+      fr_chunk_sum x[kLoads];
+#pragma unroll
+      for (uint32_t k = 0; k < kLoads; k++) {
+        const uint64_t g = uint64_t(d.slot) + (j + k * L < d.n ? j + k * L : d.n - 1);
+        x[k] = p[(g & 7) * stride + (g >> 3)];
+      }
+#pragma unroll
+      for (uint32_t k = 0; k < kLoads; k++) {
+        s += j + k * L < d.n ? x[k].sum : 0;
+        ws += j + k * L < d.n ? x[k].wsum : 0;
+      }
     }
   }
 #pragma unroll
@@ -844,7 +856,7 @@ int step(const AdamwStepArgs& a, hipStream_t st) {
     hipLaunchKernelGGL(kernel, dim3(a.n_scales + (a.n_folds + per - 1) / per), dim3(256), 0, st, a.folds, a.n_folds,
                        a.scales, a.n_scales, a.walk.stride, a.parts, static_cast<const uint8_t*>(a.state), a.sums);
   };
-  if (tiles >= 64) fold(k_adamw_fold<64>, 64);
+  if (tiles >= 256) fold(k_adamw_fold<64>, 64);
   else fold(k_adamw_fold<16>, 16);
   return int(hipGetLastError());
 }
