@@ -29,11 +29,11 @@
 //     forms of root and quotient where the operands allow them, one scale a
 //     wave (so that it is a scalar), codes rounded in place in the top bytes of
 //     the words they are packed from: 83 -> 67 instructions an element, 2.92 ->
-//     2.55-2.73 ms by allocation, 5.9-6.3 TB/s.  The vector units are then busy
+//     2.62-2.67 ms, 6.1 TB/s.  The vector units are then busy
 //     for two thirds of it.
 //   * Sums are folded by the wave that made them (wave_totals) and left 64 bytes
 //     a tile for a second kernel: a step with them takes 4.53 ms, where the step
-//     and a checksum of the state take 6.3 (8 bits: 2.90 and 3.8).
+//     and a checksum of the state take 6.3 (8 bits: 2.85 and 3.8).
 //   * No release and acquire between workgroups (finish_norm).
 //
 // The arithmetic is that of the header, operation by operation: no contraction
@@ -63,10 +63,17 @@ struct Tile {
   uint32_t place;
 };
 
-// The tile of workgroup g.
-template <int T>
-__device__ __forceinline__ Tile tile_of(const AdamwWalk& w, const AdamwRec* recs, uint64_t g) {
+// The tile of workgroup `block`: the slot of its own number or, with kRun > 1,
+// one of kRun slots in order that the workgroups of one die take (workgroup b
+// runs on die b mod 8), so that fewer lines of scales have parts in several L2s.
+template <int T, int kRun>
+__device__ __forceinline__ Tile tile_of(const AdamwWalk& w, const AdamwRec* recs, uint32_t block) {
   Tile t;
+  uint64_t g = block;
+  if constexpr (kRun > 1) {
+    const uint32_t i = block % (8 * kRun), from = block - i;
+    if (from + 8 * kRun <= uint32_t(w.n)) g = from + i % 8 * kRun + i / 8;
+  }
   const uint64_t at = (g & 7) * w.stride + (g >> 3);
   const uint64_t slot = w.d[at];
   t.r = recs[slot >> 32];
@@ -511,13 +518,13 @@ __device__ __forceinline__ void step_tile(const StepCtx& t, u64 (&s)[kSummed], u
   }
 }
 
-template <bool kEight, bool kSums, int B, int U>
+template <bool kEight, bool kSums, int B, int U, int kRun>
 __global__ __launch_bounds__(B) void k_adamw(const AdamwRec* __restrict__ recs, AdamwWalk walk,
                                              uint8_t* __restrict__ state, const uint8_t* __restrict__ grads,
                                              const fr_adamw_hyper* __restrict__ hyper,
                                              const fr_grad_stats* __restrict__ stats, uint64_t C,
                                              fr_chunk_sum* __restrict__ parts) {
-  const Tile t = tile_of<B * U * 4>(walk, recs, blockIdx.x);
+  const Tile t = tile_of<B * U * 4, kRun>(walk, recs, blockIdx.x);
   StepCtx c;
   c.n = t.n;
   c.hyper = hyper[t.r.group];
@@ -813,10 +820,10 @@ __device__ __forceinline__ void convert_tile(const ConvertCtx& t) {
   }
 }
 
-template <bool k8To, int B, int U>
+template <bool k8To, int B, int U, int kRun>
 __global__ __launch_bounds__(B) void k_convert(const AdamwRec* from_recs, const AdamwRec* to_recs, AdamwWalk walk,
                                                const uint8_t* from, uint8_t* to, uint32_t seed) {
-  const Tile t = tile_of<B * U * 4>(walk, to_recs, blockIdx.x);
+  const Tile t = tile_of<B * U * 4, kRun>(walk, to_recs, blockIdx.x);
   const AdamwRec f = from_recs[walk.d[t.place] >> 32];
   const bool f8 = f.at[kScale1] != kNone;
   const uint64_t b0 = t.e0 / FR_ADAMW_BLOCK;
@@ -844,9 +851,9 @@ __global__ __launch_bounds__(B) void k_convert(const AdamwRec* from_recs, const 
 template <bool kEight, bool kSums>
 int step(const AdamwStepArgs& a, hipStream_t st) {
   constexpr AdamwShape s = kSums ? kSumShape[kEight] : kStepShape[kEight];
-  hipLaunchKernelGGL((k_adamw<kEight, kSums, s.B, s.U>), dim3(uint32_t(a.walk.n)), dim3(s.B), s.lds, st, a.recs, a.walk,
-                     static_cast<uint8_t*>(a.state), static_cast<const uint8_t*>(a.grads), a.hyper, a.stats, a.C,
-                     a.parts);
+  hipLaunchKernelGGL((k_adamw<kEight, kSums, s.B, s.U, s.run>), dim3(uint32_t(a.walk.n)), dim3(s.B), s.lds, st, a.recs,
+                     a.walk, static_cast<uint8_t*>(a.state), static_cast<const uint8_t*>(a.grads), a.hyper, a.stats,
+                     a.C, a.parts);
   const int e = int(hipGetLastError());
   if (e != 0 || !kSums || a.n_folds == 0) return e;
   // tiles of the longest chunks that are fed by tiles: parameters', or codes'
@@ -864,7 +871,7 @@ int step(const AdamwStepArgs& a, hipStream_t st) {
 template <bool kEight>
 int convert(const AdamwConvertArgs& a, hipStream_t st) {
   constexpr AdamwShape s = kConvertShape[kEight];
-  hipLaunchKernelGGL((k_convert<kEight, s.B, s.U>), dim3(uint32_t(a.walk.n)), dim3(s.B), s.lds, st, a.from_recs,
+  hipLaunchKernelGGL((k_convert<kEight, s.B, s.U, s.run>), dim3(uint32_t(a.walk.n)), dim3(s.B), s.lds, st, a.from_recs,
                      a.to_recs, a.walk, static_cast<const uint8_t*>(a.from), static_cast<uint8_t*>(a.to), a.seed);
   return int(hipGetLastError());
 }
