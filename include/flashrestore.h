@@ -555,10 +555,11 @@ typedef struct fr_adamw_info {
  * FR_E_INVAL: an index outside the table, an entry of the wrong dtype or
  * numel, a group that does not exist, one scale without the other, unknown
  * flags; FR_E_ALIGN: a gradient offset not a multiple of 16; FR_E_RANGE: a
- * gradient past its arena; FR_E_OVERLAP: the src ranges of two entries that
- * the step writes overlap, or one entry is named twice (gradients may
- * overlap).  The plan need not outlive the optimizer.  Synchronous, like
- * fr_plan_create; create optimizers outside graph capture. */
+ * gradient past its arena, or n_counters and 2,048 for each tensor at 2^34 or
+ * above in all; FR_E_OVERLAP: the src ranges of two entries that the step
+ * writes overlap, or one entry is named twice (gradients may overlap).  The
+ * plan need not outlive the optimizer.  Synchronous, like fr_plan_create;
+ * create optimizers outside graph capture. */
 int fr_adamw_create(const fr_plan* plan, const fr_adamw_tensor* tensors, uint32_t n,
                     uint32_t n_groups, uint64_t grad_arena_bytes, fr_adamw** out);
 int fr_adamw_get_info(const fr_adamw* opt, fr_adamw_info* out);

@@ -134,7 +134,9 @@ int validate(const fr_tensor_desc* table, uint32_t n_entries, const Layout& L, u
   for (size_t i = 1; i < written.size(); i++)
     if (written[i].first < written[i - 1].last) return FR_E_OVERLAP;
   std::sort(out->moments.begin(), out->moments.end());
-  if (info.n_counters / 256 + n >= (uint64_t(1) << 31)) return FR_E_RANGE;  // workgroups of a launch
+  // a launch has fewer than 2^32 threads: a wave for each tile of 256 elements,
+  // or a workgroup for each chunk of scales, of which a tensor has two
+  if (info.n_counters / 256 + 8 * uint64_t(n) >= (uint64_t(1) << 26)) return FR_E_RANGE;
   return FR_OK;
 }
 

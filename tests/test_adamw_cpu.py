@@ -92,6 +92,16 @@ def test_refusals_of_overlaps_and_scales():
     assert _status(t, r, ab, gb, groups=0) == -1
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_refusal_of_more_threads_than_a_launch_has(bits):
+    counters = (1 << 34) - 2048 - 1024  # with the tensor's own 2,048 just below 2^34
+    for numel, code in ((counters, 0), (counters + 1, -3)):
+        t, r, ab, gb = F.fr_adamw_state_table([numel], bits)
+        assert _status(t, r, ab, gb, C=1 << 20) == code
+    t, r, ab, gb = F.fr_adamw_state_table([1 << 33, 1 << 32], bits)
+    assert _status(t, r, ab, gb, C=1 << 20) == 0
+
+
 def test_create_without_a_plan_or_output():
     assert F._lib.fr_adamw_create(None, None, 0, 0, 0, None) == -1
     assert F._lib.fr_adamw_get_info(None, None) == -1 and F._lib.fr_adamw_destroy(None) == 0
