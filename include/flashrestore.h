@@ -540,9 +540,9 @@ typedef struct fr_adamw_info {
   uint64_t arena_bytes;      /* of the state: the plan's src_arena_bytes */
   uint64_t sums_chunks;      /* chunks whose sums a step writes (0 where the
                                 plan's chunks are below FR_ADAMW_MIN_SUM_CHUNK) */
-  uint64_t device_bytes;     /* device memory of the optimizer itself: 0.3 to 0.4
-                                bytes an element with sums, else 0.05 (0 for a
-                                query) */
+  uint64_t device_bytes;     /* device memory of the optimizer itself: 0.3 bytes
+                                an element (0.15 in 8 bits) with sums, else
+                                0.05 (0 for a query) */
   int64_t device;            /* -1 for a query */
 } fr_adamw_info;
 

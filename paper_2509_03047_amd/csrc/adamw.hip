@@ -28,8 +28,8 @@
 //   * Instructions, in 8 bits: hardware conversions from fp8 and to bf16, short
 //     forms of root and quotient where the operands allow them, one scale a
 //     wave (so that it is a scalar), codes rounded in place in the top bytes of
-//     the words they are packed from: 83 -> 67 instructions an element, 2.92 ->
-//     2.62-2.67 ms, 6.1 TB/s.  The vector units are then busy
+//     the words they are packed from: 83 -> 70 instructions an element, 2.92 ->
+//     2.55-2.67 ms by allocation, 6.0-6.3 TB/s.  The vector units are then busy
 //     for two thirds of it.
 //   * Sums are folded by the wave that made them (wave_totals) and left 64 bytes
 //     a tile for a second kernel: a step with them takes 4.53 ms, where the step
