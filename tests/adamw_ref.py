@@ -133,7 +133,7 @@ class State:
                 self.table[k]["src_offset"] = self.table[k]["dst_offset"] = pos
                 pos += -(-int(self.table[k]["numel"]) * (2 if self.table[k]["dtype"] == F.FR_BF16 else 4) // 16) * 16
             self.arena_bytes = pos + 48
-        self.grad_dtype, self.groups = grad_dtype, groups
+        self.groups = groups
         self.base = np.concatenate([[0], np.cumsum([-(-n // SPAN) * SPAN for n in self.numel])])
         self.arena = np.full(max(self.arena_bytes, 1), 0xA5, np.uint8)
         self.grads = np.full(max(self.grad_bytes, 1), 0xFF, np.uint8)  # bf16 and fp32 NaN between the tensors
@@ -187,12 +187,12 @@ class State:
 
     def set_grad(self, k, g):
         o = int(self.rows[k]["grad_offset"])
-        b = (rne_bf16(g) if self.grad_dtype == F.FR_BF16 else np.ascontiguousarray(g, f32)).view(np.uint8)
+        b = (rne_bf16(g) if self.rows[k]["grad_dtype"] == F.FR_BF16 else np.ascontiguousarray(g, f32)).view(np.uint8)
         self.grads[o:o + b.size] = b
 
     def grad(self, k):
         o, n = int(self.rows[k]["grad_offset"]), self.numel[k]
-        if self.grad_dtype == F.FR_BF16:
+        if self.rows[k]["grad_dtype"] == F.FR_BF16:
             return from_bf16(self.grads[o:o + 2 * n].view(np.uint16))
         return self.grads[o:o + 4 * n].view(f32).copy()
 

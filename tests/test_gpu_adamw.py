@@ -102,6 +102,26 @@ def test_steps_give_the_models_bits(bits, grad, scaled, seed):
         assert first_difference(s, d.host(), s.arena) is None, step
 
 
+@pytest.mark.parametrize("bits", [32, 8, "both"])
+def test_gradients_of_both_types_in_one_step(bits):
+    numel = RAGGED + [20_000, 70_001]
+    s = R.State(numel, [32, 8] * (len(numel) // 2) if bits == "both" else bits, F.FR_F32, groups=2, seed=14, shuffle=True)
+    for k in range(0, len(numel), 3):
+        g = s.grad(k)
+        s.rows["grad_dtype"][k] = F.FR_BF16
+        s.set_grad(k, g)
+    d, h = Dev(s), two_groups(seed=9)
+    got, want = d.plan.empty_sums(), d.plan.empty_sums()
+    d.opt.grad_norm(d.grads, 1e-3, d.stats)
+    sq = math.fsum(float(x) * float(x) for k in range(len(numel)) for x in s.grad(k))
+    assert abs(float(d.stats[0]) - sq) <= sum(numel) * 2.0 ** -52 * sq
+    d.opt.step(d.state, d.grads, hyper_dev(h), d.stats, got)
+    s.arena = s.stepped(h, d.stats.view(torch.float32)[3].item())
+    assert first_difference(s, d.host(), s.arena) is None
+    d.plan.checksum_state(d.state, want)
+    assert np.array_equal(sums_host(got, d.plan.n_chunks), sums_host(want, d.plan.n_chunks))
+
+
 def test_step_in_64_bits():
     """Against AdamW in 64 bits, by the bounds derived in tests/test_adamw_cpu.py."""
     u = 2.0 ** -24
