@@ -483,7 +483,9 @@ int fr_unpack_flagged(const fr_plan* plan, const void* payload, uint64_t payload
  *   Norm.  sum_sq = the sum of the squares of all counted gradients in 64
  *     bits, in an order that depends on the table alone; norm = sqrt(sum_sq)
  *     rounded to fp32; scale = max_norm / norm (fp32) where norm > max_norm,
- *     else 1; nonfinite = 1 and scale = 0 where sum_sq is not finite, else 0. */
+ *     else 1; nonfinite = 1 and scale = 0 where sum_sq is not finite, else 0.
+ *     Where the root of a finite sum_sq is past fp32's range, norm is infinity
+ *     and scale the quotient by the root in 64 bits, rounded to fp32. */
 
 #define FR_ADAMW_BLOCK 256
 #define FR_ADAMW_SPAN 1024

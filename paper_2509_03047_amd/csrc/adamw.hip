@@ -637,12 +637,16 @@ __global__ __launch_bounds__(256) void k_adamw_fold(const AdamwFold* folds, uint
 
 // --------------------------------------------------------------------- norm
 
+// (A norm past fp32's range, of gradients that are finite, still has a scale: a
+// quotient of infinity would step with gradients of zero.)
 __device__ __forceinline__ void set_stats(double sum_sq, float max_norm, fr_grad_stats* out) {
   const bool fine = __builtin_isfinite(sum_sq);
-  const float norm = float(__builtin_sqrt(sum_sq));
+  const double root = __builtin_sqrt(sum_sq);
+  const float norm = float(root);
+  const float clip = __builtin_isfinite(norm) ? max_norm / norm : float(double(max_norm) / root);
   out->sum_sq = sum_sq;
   out->norm = norm;
-  out->scale = !fine ? 0.0f : norm > max_norm ? max_norm / norm : 1.0f;
+  out->scale = !fine ? 0.0f : norm > max_norm ? clip : 1.0f;
   out->nonfinite = fine ? 0 : 1;
 }
 
