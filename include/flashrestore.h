@@ -498,7 +498,8 @@ typedef struct fr_adamw_tensor {
   uint64_t grad_offset; /* from the gradient arena base; multiple of 16 */
   uint32_t grad_dtype;  /* FR_F32 or FR_BF16 */
   uint32_t group;       /* its row of the hyperparameters */
-  int32_t param;        /* FR_BF16 entry that gets RNE(master), or -1 */
+  int32_t param;        /* FR_BF16 entry that gets RNE(master), or -1; if the
+                           table derives it, then from master */
   int32_t master;       /* FR_F32 entry; its numel is the tensor's */
   int32_t m, v;         /* FR_F32 entries: numel values each, or (8 bits)
                            ceil(numel / 4) words that hold the codes in order */
@@ -555,12 +556,17 @@ typedef struct fr_adamw_info {
  *   n_groups          rows of hyperparameters that a step will be given
  *   grad_arena_bytes  size of the gradient arena
  * FR_E_INVAL: an index outside the table, an entry of the wrong dtype or
- * numel, a group that does not exist, one scale without the other, unknown
+ * numel, a parameter that the table derives from another entry than its
+ * master, a group that does not exist, one scale without the other, unknown
  * flags; FR_E_ALIGN: a gradient offset not a multiple of 16; FR_E_RANGE: a
  * gradient past its arena, or n_counters and 2,048 for each tensor at 2^34 or
  * above in all; FR_E_OVERLAP: the src ranges of two entries that the step
- * writes overlap, or one entry is named twice (gradients may overlap).  The
- * plan need not outlive the optimizer.  Synchronous, like fr_plan_create;
+ * writes overlap, or one entry is named twice (gradients may overlap).
+ *   An entry that the table derives from one that a step writes, and that is
+ * not that tensor's param, is not written: it is the caller's to bring up to
+ * date before the state is packed, as a restore derives it anew and a donor
+ * with the old one would differ from what it restored.
+ *   The plan need not outlive the optimizer.  Synchronous, like fr_plan_create;
  * create optimizers outside graph capture. */
 int fr_adamw_create(const fr_plan* plan, const fr_adamw_tensor* tensors, uint32_t n,
                     uint32_t n_groups, uint64_t grad_arena_bytes, fr_adamw** out);

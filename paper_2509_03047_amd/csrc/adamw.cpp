@@ -75,7 +75,7 @@ int validate(const fr_tensor_desc* table, uint32_t n_entries, const Layout& L, u
   info.grad_arena_bytes = grad_bytes;
   info.arena_bytes = arena_bytes;
   info.device = -1;
-  bool twice = false;
+  bool twice = false, strange = false;
   for (uint32_t k = 0; k < n; k++) {
     const fr_adamw_tensor& d = t[k];
     if (d.reserved || (d.flags & ~uint32_t(FR_GRAD_NOT_COUNTED)) || d.group >= n_groups) return FR_E_INVAL;
@@ -104,6 +104,9 @@ int validate(const fr_tensor_desc* table, uint32_t n_entries, const Layout& L, u
       }
       const uint32_t e = uint32_t(want[j].entry);
       if (e >= n_entries || table[e].dtype != want[j].dtype || table[e].numel != want[j].numel) return FR_E_INVAL;
+      // (a restore derives the parameter anew: from the master that a step writes
+      // it from, or not at all; of none there is nothing that could differ)
+      if (j == kParam) strange |= numel && table[e].derive_from != -1 && table[e].derive_from != d.master;
       twice |= named[e] != 0;
       named[e] = 1;
       r.at[j] = table[e].src_offset;
@@ -133,6 +136,7 @@ int validate(const fr_tensor_desc* table, uint32_t n_entries, const Layout& L, u
   std::sort(written.begin(), written.end());
   for (size_t i = 1; i < written.size(); i++)
     if (written[i].first < written[i - 1].last) return FR_E_OVERLAP;
+  if (strange) return FR_E_INVAL;
   std::sort(out->moments.begin(), out->moments.end());
   // a launch has fewer than 2^32 threads: a wave for each tile of 256 elements,
   // or a workgroup for each chunk of scales, of which a tensor has two

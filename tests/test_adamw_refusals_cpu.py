@@ -1,0 +1,48 @@
+"""Optimizers and states that look right by their sizes alone and are not (CPU)."""
+import numpy as np
+import pytest
+
+from paper_2509_03047_amd import flashrestore as F
+
+INVAL = -1
+
+
+def _status(t, r, ab, gb, C=4096):
+    try:
+        F.fr_adamw_query(t, C, ab, r, 1, gb)
+        return 0
+    except F.FlashRestoreError as e:
+        return e.status
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_parameter_is_derived_from_its_own_master(bits):
+    """A restore derives a parameter from the master that the table names; a step that wrote it from another one
+    would leave a state that its restored copy differs from."""
+    t, r, ab, gb = F.fr_adamw_state_table([300, 300], bits)
+    assert _status(t, r, ab, gb) == 0
+    swapped = r.copy()
+    swapped["param"] = r["param"][::-1]
+    assert _status(t, swapped, ab, gb) == INVAL
+    swapped = r.copy()
+    swapped["master"] = r["master"][::-1]
+    assert _status(t, swapped, ab, gb) == INVAL
+    one = r[:1].copy()
+    one["param"] = r["param"][1]  # the other tensor, which no step writes
+    assert _status(t, one, ab, gb) == INVAL
+    one["param"] = -1  # an image that the caller brings up to date
+    assert _status(t, one, ab, gb) == 0
+    plain = t.copy()
+    plain["derive_from"] = -1  # images that are sent, not derived: any master's
+    assert _status(plain, r, ab, gb) == 0
+    swapped = r.copy()
+    swapped["param"] = r["param"][::-1]
+    assert _status(plain, swapped, ab, gb) == 0
+
+
+def test_a_moment_in_the_masters_place():
+    """The master's index names a moment's entry of the same size and the moment's the master's."""
+    for numel in (300, 0):  # (an empty parameter has nothing to differ in)
+        t, r, ab, gb = F.fr_adamw_state_table([numel], 32)
+        r["master"], r["m"] = int(r["m"][0]), int(r["master"][0])
+        assert _status(t, r, ab, gb) == (INVAL if numel else 0)
