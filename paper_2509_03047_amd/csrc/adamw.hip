@@ -712,10 +712,11 @@ __device__ __forceinline__ void finish_norm(double sum, double* parts, uint32_t*
                                             fr_grad_stats* stats) {
   __shared__ bool last;
   if (threadIdx.x == 0) {
-    (void)__hip_atomic_exchange(reinterpret_cast<unsigned long long*>(parts + blockIdx.x),
-                                __builtin_bit_cast(unsigned long long, sum), __ATOMIC_RELAXED,
-                                __HIP_MEMORY_SCOPE_AGENT);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    const unsigned long long before = __hip_atomic_exchange(
+        reinterpret_cast<unsigned long long*>(parts + blockIdx.x), __builtin_bit_cast(unsigned long long, sum),
+        __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    // (unused, it would be compiled to the form without a return)
+    asm volatile("s_waitcnt vmcnt(0)" ::"v"(before) : "memory");
     const uint32_t lines = (gridDim.x + kNormPerLine - 1) / kNormPerLine, line = blockIdx.x % lines;
     last = gridDim.x <= kNormOneLine
                ? arrive_last(arrived, 0, gridDim.x)
