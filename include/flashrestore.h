@@ -587,7 +587,8 @@ int fr_adamw_query(const fr_tensor_desc* table, uint32_t n_entries, uint64_t chu
  *   numel   n element counts
  *   bits    n moment widths, 32 or 8; NULL: all 32
  * tensors (NULL or n) gets the descriptors, group 0.  With table == NULL only
- * the sizes are set; FR_E_RANGE if cap < *n_entries. */
+ * the sizes are set; FR_E_RANGE if cap < *n_entries, and for a tensor of more
+ * than 2^48 elements, 2^58 in all or 2^31 entries. */
 int fr_adamw_state_table(const uint64_t* numel, const uint8_t* bits, uint32_t n,
                          uint32_t grad_dtype, fr_tensor_desc* table, uint32_t cap,
                          uint32_t* n_entries, fr_adamw_tensor* tensors, uint64_t* arena_bytes,

@@ -364,13 +364,15 @@ extern "C" int fr_adamw_state_table(const uint64_t* numel, const uint8_t* bits, 
   if (!n_entries || !arena_bytes || !grad_bytes || (n && !numel)) return FR_E_INVAL;
   if (grad_dtype != FR_F32 && grad_dtype != FR_BF16) return FR_E_INVAL;
   const uint64_t gsize = grad_dtype == FR_F32 ? 4 : 2;
-  uint64_t want = 0, off = 0, goff = 0;
+  uint64_t want = 0, elements = 0, off = 0, goff = 0;
   for (uint32_t k = 0; k < n; k++) {
     if (bits && bits[k] != 32 && bits[k] != 8) return FR_E_INVAL;
     if (numel[k] > (uint64_t(1) << 48)) return FR_E_RANGE;
     want += bits && bits[k] == 8 ? 6 : 4;
+    elements += numel[k];
+    // (at most 14 bytes each, and 90 for a tensor's last ones: below 2^62)
+    if (want > 0x7FFFFFFFu || elements > (uint64_t(1) << 58)) return FR_E_RANGE;
   }
-  if (want > 0x7FFFFFFFu) return FR_E_RANGE;
   *n_entries = uint32_t(want);
   if (table && cap < want) return FR_E_RANGE;
   uint32_t e = 0;

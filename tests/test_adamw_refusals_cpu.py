@@ -4,7 +4,7 @@ import pytest
 
 from paper_2509_03047_amd import flashrestore as F
 
-INVAL = -1
+INVAL, RANGE = -1, -3
 
 
 def _status(t, r, ab, gb, C=4096):
@@ -46,3 +46,22 @@ def test_a_moment_in_the_masters_place():
         t, r, ab, gb = F.fr_adamw_state_table([numel], 32)
         r["master"], r["m"] = int(r["m"][0]), int(r["master"][0])
         assert _status(t, r, ab, gb) == (INVAL if numel else 0)
+
+
+def test_states_whose_sizes_pass_64_bits():
+    """5,000 tensors of 2^48 elements are 2e19 bytes of state: refused, where the sum wrapped around 2^64 before."""
+    with pytest.raises(F.FlashRestoreError) as ei:
+        F.fr_adamw_state_table([1 << 48] * 5000)
+    assert ei.value.status == RANGE
+    for bits in (32, 8):
+        n = 1 << 10  # 2^58 elements in all are the most
+        t, r, ab, gb = F.fr_adamw_state_table([1 << 48] * n, bits, F.FR_F32)
+        size = (2 + 4 + 4 + 4) << 48 if bits == 32 else (2 + 4 + 1 + 1) * (1 << 48) + 2 * ((1 << 48) // 256 * 4)
+        assert ab == n * size and gb == n * (4 << 48)
+        assert int(t[-1]["src_offset"]) < ab and int(r[-1]["grad_offset"]) == (n - 1) * (4 << 48)
+        with pytest.raises(F.FlashRestoreError) as ei:
+            F.fr_adamw_state_table([1 << 48] * n + [1], bits, F.FR_F32)
+        assert ei.value.status == RANGE
+    with pytest.raises(F.FlashRestoreError) as ei:
+        F.fr_adamw_state_table([(1 << 48) + 1])
+    assert ei.value.status == RANGE
