@@ -561,6 +561,8 @@ def adamw_hyper(groups, step: int) -> np.ndarray:
     """A fr_adamw_hyper array for step `step` (1 for the first): a dict for each
     group, with lr and, where they differ from these, betas (0.9, 0.999), eps
     1e-8, weight_decay 0 and seed 0 (the seed of stochastic rounding)."""
+    if step < 1:
+        raise ValueError(f"step {step}: steps count from 1")
     h = np.zeros(len(groups), HYPER_DTYPE)
     for row, g in zip(h, groups):
         unknown = set(g) - {"lr", "betas", "eps", "weight_decay", "seed"}

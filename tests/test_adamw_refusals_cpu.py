@@ -65,3 +65,12 @@ def test_states_whose_sizes_pass_64_bits():
     with pytest.raises(F.FlashRestoreError) as ei:
         F.fr_adamw_state_table([(1 << 48) + 1])
     assert ei.value.status == RANGE
+
+
+def test_hyperparameters_of_no_step():
+    """Steps count from 1: the corrections of step 0 would be 0, and a step would divide by them."""
+    for step in (0, -1, np.int64(0)):
+        with pytest.raises(ValueError, match="step"):
+            F.adamw_hyper([dict(lr=1e-3)], step)
+    h = F.adamw_hyper([dict(lr=1e-3)], 1)
+    assert h[0]["bias1"] == np.float32(1 - 0.9) and h[0]["bias2"] == np.float32(1 - 0.999)
