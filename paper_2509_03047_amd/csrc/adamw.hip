@@ -78,8 +78,9 @@ __device__ __forceinline__ Tile tile_of(const AdamwWalk& w, const AdamwRec* recs
   const uint64_t slot = w.d[at];
   t.r = recs[slot >> 32];
   t.e0 = uint64_t(uint32_t(slot)) * T;
-  // (in 32 bits: a scalar 64-bit comparison has no instruction, and its detour
-  // by a vector one has been followed by a select on a stale condition)
+  // (in 32 bits: of `left < T ? left : T` in 64, which the callers' branch on a
+  // whole tile compares again, clang 22 of ROCm 7.2.0 makes a vector comparison
+  // and, behind the branch, a scalar select on the carry of an earlier sum)
   const uint32_t j = uint32_t(slot), whole = uint32_t(t.r.numel / T);
   t.n = j < whole ? uint32_t(T) : uint32_t(t.r.numel) % T;
   t.place = uint32_t(at);
