@@ -621,7 +621,9 @@ int fr_grad_scale(const fr_adamw* opt, float max_norm, fr_grad_stats* stats, hip
  *           those of the tensors' chunks get FRSUM-128 of the chunk after the
  *           step (what fr_checksum_state gives for it), others are left alone;
  *           FR_E_INVAL where the plan's chunks are below
- *           FR_ADAMW_MIN_SUM_CHUNK bytes */
+ *           FR_ADAMW_MIN_SUM_CHUNK bytes.  (In chunks of 64 MiB and more, or
+ *           that hold a small state's largest tensors whole, a step without
+ *           sums and fr_checksum_state may take less time.) */
 int fr_adamw_step(const fr_adamw* opt, void* state, const void* grads,
                   const fr_adamw_hyper* hyper, const fr_grad_stats* stats, fr_chunk_sum* sums,
                   hipStream_t stream);

@@ -88,28 +88,33 @@ struct AdamwConvertArgs {
 
 // How a kernel takes its work: workgroups of B threads with U groups of four
 // elements each, the LDS a launch asks for to bound how many of them a compute
-// unit (160 KB) holds (adamw.hip says why, and what a step's measured), and how
-// many consecutive tiles one die takes.
+// unit holds (adamw.hip says why, and what a step's measured), and how many
+// consecutive tiles one die takes.  A compute unit gives its 160 KB out in blocks
+// of 1,280 bytes, so that a request for 14,800 of them leaves room for 10
+// workgroups (so many of them sleep side by side; the runtime's occupancy query
+// does not round up, and says 11).
 struct AdamwShape {
   uint32_t B, U, lds, run;
   constexpr uint32_t tile() const { return B * U * 4; }
 };
-// Times are of an 8B model's share, 1.0e9 elements.
-// By form, 32 bits and 8: 11 and 24 waves a compute unit.  (8 bits: U = 1, no
-// bound 2.78-2.81 ms; U = 2, 20 waves 2.78, 24 waves 2.69-2.74; U = 4, 16 waves 2.70-2.73.
-// Two tiles a run 2.62-2.67, four 2.68-2.72, eight 2.83-2.87, when the dies' windows
-// drift apart; in 32 bits one 4.28-4.32, two 4.38-4.46.)
+// Times are of an 8B model's share, 1.0e9 elements, in three allocations.
+// By form, 32 bits and 8: 10 and 21 waves a compute unit.  (8 bits, U = 2: 12 waves
+// 2.68-2.72 ms, 16 2.59-2.64, 21 2.62-2.69, no bound 2.66-2.72; U = 1: 21 2.64-2.66, 25
+// 2.58-2.69; U = 4: 11 2.61-2.71.  One tile a run 2.55-2.76, two 2.62-2.69, four
+// 2.67-2.69, eight 2.66-2.89, when the dies' windows drift apart; in 32 bits one
+// 4.32-4.48, two 4.40-4.49.)
 constexpr AdamwShape kStepShape[2] = {{64, 1, 14800, 1}, {64, 2, 6800, 2}};
-// Steps that also sum: one wave, which folds its own sums; 16 and 32 waves.  (32
-// bits: 12 waves 4.97-5.04 ms, 14 4.79-4.87, 16 4.49-4.53, 20 4.50-4.54; U = 2, 8 waves 4.80,
-// 12 4.53-4.66.  8 bits: U = 1 3.03-3.19; U = 2, 16 waves 3.20-3.34, 24 2.96-3.06, no bound
-// 2.84-3.00, where the step and a checksum of the state take 3.8.)
+// Steps that also sum: one wave, which folds its own sums; 16 and, as many as their
+// registers allow, 24 waves.  (32 bits: 12 waves 4.78-4.85 ms, 14 4.61-4.66, 16
+// 4.53-4.61, 21 4.57-4.69; U = 2: 10 waves 4.51-4.66, 12 4.48-4.72.  8 bits: U = 1
+// 2.91-2.93; U = 2: 16 waves 3.03-3.07, 21 2.82-2.85, no bound 2.76-2.78, where the step
+// and a checksum of the state take 3.8.)
 constexpr AdamwShape kSumShape[2] = {{64, 1, 10200, 1}, {64, 2, 0, 1}};
-// By the form written: 12 workgroups of two waves and 1,024 elements.  (To 8 bits:
-// 64 x 2, 24 a compute unit 1.63-1.64 ms, 128 x 2, 12 1.62.  To 32: 64 x 2, 24 1.63-1.70,
-// 128 x 2, 12 1.63-1.71, 64 x 8, 5 1.60-1.65, but of 2,000 ragged tensors 69 us where the
-// smaller tiles take 61.  Two tiles a run, side by side on the same memory: to 8 bits
-// 1.59-1.61 instead of 1.61-1.64, to 32 1.65-1.69 instead of 1.68-1.70.)
+// By the form written: 11 workgroups of two waves and 1,024 elements.  (To 8 bits:
+// 64 x 2, 21 a compute unit 1.60-1.61 ms, 128 x 2, 11 1.59-1.61.  To 32: 64 x 2, 21
+// 1.64-1.67, 12 1.59-1.61, 128 x 2, 11 1.63-1.68, 64 x 8, 5 1.59-1.64, but of 2,000 ragged
+// tensors 69 us where the smaller tiles take 61.  One tile a run instead of two:
+// to 8 bits 1.59-1.61, to 32 1.63-1.71.)
 constexpr AdamwShape kConvertShape[2] = {{128, 2, 13500, 2}, {128, 2, 13500, 2}};
 constexpr uint32_t kNormBytes = 16384;  // of gradients a workgroup of a norm takes (8 KiB: 374 us instead of 304)
 // A norm of more workgroups than kNormOne adds up their sums by a second launch

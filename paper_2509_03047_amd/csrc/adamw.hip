@@ -15,25 +15,32 @@
 //     elements on each compute unit the step of an 8B model's share (1.0e9
 //     elements, bf16 gradients) ran at 6.3 TB/s in some allocations and 5.5 in
 //     most, whatever the arrays' offsets to each other; the smaller the windows,
-//     the smaller the gap.  One wave and 256 elements a workgroup
-//     and 11 workgroups a compute unit close it: 4.29 ms, 6.55 TB/s, in all (10:
-//     4.32; 13: 4.34; 16: 4.45-4.51; 128 threads, 6 a compute unit: 4.33-4.51;
-//     256 threads, 3: 4.67-4.82).  The number is set by LDS that the launch asks
-//     for and nothing uses, as there is no other limit short of the registers'.
+//     the smaller the gap.  One wave and 256 elements a workgroup and 10
+//     workgroups a compute unit leave little of it: 4.32-4.48 ms in three
+//     allocations, 6.3-6.5 TB/s (9: 4.38-4.50; 12: 4.33-4.53; 16: 4.45-4.63; no
+//     bound: 4.73-4.77; 512 elements a wave, 8 to 32: 4.42-5.07; 128 threads, 5 a
+//     compute unit: 4.39-4.60; 256 threads, 3: 4.35-4.59).  The number is set by
+//     LDS that the launch asks for and nothing uses, as there is no other limit
+//     short of the registers' (adamw.h).
 //     With less work in flight the chain of dependent loads (slot, record,
 //     hyperparameters, data) is what a tile waits for, so everything that does
 //     not depend on the data is loaded before it, and computed behind it.
 //     The other kernels have more instructions or fewer bytes a tile, which
-//     takes more of them; their numbers (adamw.h) are the best of similar sweeps.
+//     takes more of them; their numbers (adamw.h) are from similar sweeps.
 //   * Instructions, in 8 bits: hardware conversions from fp8 and to bf16, short
 //     forms of root and quotient where the operands allow them, one scale a
 //     wave (so that it is a scalar), codes rounded in place in the top bytes of
 //     the words they are packed from: 83 -> 70 instructions an element, 2.92 ->
-//     2.55-2.67 ms by allocation, 6.0-6.3 TB/s.  The vector units are then busy
+//     2.55-2.75 ms by allocation, 5.9-6.3 TB/s.  The vector units are then busy
 //     for two thirds of it.
 //   * Sums are folded by the wave that made them (wave_totals) and left 64 bytes
-//     a tile for a second kernel: a step with them takes 4.53 ms, where the step
-//     and a checksum of the state take 6.3 (8 bits: 2.85 and 3.8).
+//     a tile for a second kernel: a step with them takes 4.5-4.9 ms by where the
+//     arrays lie, where the step and a checksum of the state take 6.3 (8 bits:
+//     2.8 and 3.8), in chunks of up to 16 MiB.  That kernel reads a chunk's parts
+//     with one wave at most: from 64 MiB on it outlasts the checksum of a tensor
+//     that few chunks hold (124M elements: 753 us where the two calls take 782,
+//     8 bits 584 and 499; in chunks of 256 MiB 1,330 and 822, 768 and 536), and from
+//     4 MiB on that of a small state (3.7M elements: 34 and 31, 23 and 23).
 //   * No release and acquire between workgroups (finish_norm).
 //
 // The arithmetic is that of the header, operation by operation: no contraction
@@ -306,9 +313,12 @@ __device__ __forceinline__ u32x2 to_bf16(const f32x4& x) {
 // multiply-adds), as P. Markstein, "Computation of elementary functions on the
 // IBM RISC System/6000 processor" (1990), shows: a quotient that is within one
 // unit of its last place, corrected by its residual times a correctly rounded
-// reciprocal, is correctly rounded.  The root's correction and the reciprocal
-// have been compared with the general form's for every operand of the ranges
-// below.
+// reciprocal, is correctly rounded.  (m * y may be off by up to one and a half
+// where m's mantissa is the smaller one: the 2.2e8 quotients of 24-bit numbers
+// nearest to a border, over all divisors, come out right all the same, and with
+// a reciprocal that is one unit off 5e6 of them do not.)  The tests compare
+// these, and on the device every root of three pairs of binades, the ranges'
+// ends among them, and its quotients with the numerators hardest to round.
 __device__ __forceinline__ float root_inside(float v) {  // 2^-96 <= v <= 2^126 (NaN of a negative one)
   const float y = __builtin_amdgcn_rsqf(v), g = v * y;
   return __builtin_fmaf(__builtin_fmaf(-g, g, v), 0.5f * y, g);

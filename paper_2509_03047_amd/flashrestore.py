@@ -614,7 +614,8 @@ def fr_adamw_state_table(numel, bits=None, grad_dtype: int = FR_BF16):
 
 class AdamW:
     """An optimizer over the entries of a plan's table (``fr_adamw_*``), bound
-    to the plan's device."""
+    to the plan's device.  Its calls share scratch memory and must not overlap
+    in time: those on several streams have to wait for each other."""
 
     def __init__(self, plan: Plan, tensors, n_groups: int, grad_arena_bytes: int):
         self._h = None
