@@ -639,6 +639,225 @@ int fr_adamw_step(const fr_adamw* opt, void* state, const void* grads,
 int fr_adamw_convert(const fr_adamw* from, const void* from_state, const fr_adamw* to,
                      void* to_state, uint32_t seed, hipStream_t stream);
 
+/* ------------------------------------------ orthogonalised updates (Muon) */
+
+/* The step of a state's matrices by orthogonalised momentum, beside AdamW's for
+ * everything else: a matrix's direction is brought near to the orthogonal
+ * matrix nearest to it by a few products (Newton-Schulz), and the step goes
+ * along that.  A matrix keeps a master, a parameter and one momentum.
+ *
+ * Definitions
+ *   Direction.  For each element, every operation one fp32 operation rounded to
+ *     nearest even, with the scale of the gradients (1 without stats) and the
+ *     group's hyperparameters:
+ *       x  = grad * scale
+ *       m' = momentum * m + x
+ *       d  = x + momentum * m' where nesterov is not 0, else m'
+ *   Orthogonalisation of a matrix D of rows x cols elements, row by row:
+ *       X_0     = D / (|D| + eps), |D| the root of the sum of its squares
+ *       X_(i+1) = a_i X_i + (b_i A + c_i A A) X_i,  A = X_i X_i^T
+ *     (with X_i^T X_i on the right where rows > cols) over the optimizer's
+ *     steps; the update U is the last X in bf16.  On singular values a step is
+ *     the polynomial a s + b s^3 + c s^5.  The sum of squares is kept in 64 bits,
+ *     products have fp16 operands (a power of two brings them into its range)
+ *     and fp32 sums; X itself is carried in fp32 up to the last step but two.
+ *     The updates differ from the exact ones by some 2e-3 of their norm, of
+ *     which bf16 alone makes 1.7e-3.  U depends on D, eps and the coefficients
+ *     alone, not on the other matrices nor on the launch: replicas stay
+ *     identical bit for bit.
+ *     A matrix of zeros gives zeros (eps > 0); one that holds a NaN or an
+ *     infinity gives NaN everywhere; other matrices do not feel it.
+ *   Step, rounded operation by operation like AdamW's, with the matrix's scale:
+ *       w' = w * (1 - lr * weight_decay) - u * (lr * scale)
+ *     for the master w, and the parameter is RNE(w'). */
+
+/* One matrix of the step: its entries in a plan's table (their src offsets
+ * and, for sums, chunks), its gradient and its update.  56 bytes, no padding. */
+typedef struct fr_muon_tensor {
+  uint64_t grad_offset;   /* from the gradient arena base; multiple of 16 */
+  uint64_t update_offset; /* from the update arena base (bf16); multiple of 16 */
+  uint32_t rows, cols;    /* rows * cols is the master's numel */
+  uint32_t grad_dtype;    /* FR_F32 or FR_BF16 */
+  uint32_t group;         /* its row of the hyperparameters */
+  int32_t param;          /* FR_BF16 entry that gets RNE(master), or -1; if the
+                             table derives it, then from master */
+  int32_t master;         /* FR_F32 entry */
+  int32_t m;              /* FR_F32 entry of as many values */
+  uint32_t flags;         /* 0 */
+  float scale;            /* of its update, for instance 0.2 sqrt(max(rows, cols)) */
+  uint32_t reserved;      /* 0 */
+} fr_muon_tensor;
+
+/* Hyperparameters of a group for one step (device memory).  32 bytes. */
+typedef struct fr_muon_hyper {
+  float lr, momentum, eps, weight_decay;
+  uint32_t nesterov;
+  uint32_t reserved[3];
+} fr_muon_hyper;
+
+/* One step's coefficients. */
+typedef struct fr_muon_coeffs {
+  float a, b, c;
+} fr_muon_coeffs;
+#define FR_MUON_MAX_STEPS 16
+
+typedef struct fr_muon fr_muon; /* opaque, owned by the library */
+
+typedef struct fr_muon_info {
+  uint64_t n_tensors;
+  uint64_t n_groups;
+  uint64_t n_steps;
+  uint64_t n_elements;         /* of all matrices */
+  uint64_t multiplications;    /* of one orthogonalisation, those of symmetric
+                                  products counted once */
+  uint64_t grad_arena_bytes;
+  uint64_t update_arena_bytes;
+  uint64_t arena_bytes;        /* of the state: the plan's src_arena_bytes */
+  uint64_t sums_chunks;        /* chunks whose sums direction and apply write */
+  uint64_t device_bytes;       /* device memory of the optimizer itself, some 10
+                                  bytes an element and 4 for each of a product's
+                                  (0 for a query) */
+  int64_t device;              /* -1 for a query */
+} fr_muon_info;
+
+/* Validate the matrices of an optimizer against a plan's table and build what
+ * its calls need on the plan's device (which must be current:
+ * FR_E_DEVICE_MISMATCH).
+ *   tensors   n descriptors (host memory; copied)
+ *   coeffs    n_steps (1 to FR_MUON_MAX_STEPS) steps (host memory; copied);
+ *             NULL, with n_steps = 0: five of (3.4445, -4.7750, 2.0315)
+ * Errors as of fr_adamw_create; FR_E_INVAL also for rows * cols other than the
+ * master's numel, a scale that is not finite, and coefficients that are not
+ * finite or let a singular value in [0, 1] grow past 4, or |b s^2| + |c s^4|
+ * past 64, on the way; FR_E_RANGE for a side of more than 2^20 or 2^31 elements
+ * or more, a smaller side above 2^15, 2^34 elements in all; FR_E_OVERLAP also for
+ * two updates that overlap.
+ *   The plan need not outlive the optimizer.  Synchronous; create optimizers
+ * outside graph capture. */
+int fr_muon_create(const fr_plan* plan, const fr_muon_tensor* tensors, uint32_t n, uint32_t n_groups,
+                   uint64_t grad_arena_bytes, uint64_t update_arena_bytes, const fr_muon_coeffs* coeffs,
+                   uint32_t n_steps, fr_muon** out);
+int fr_muon_get_info(const fr_muon* opt, fr_muon_info* out);
+/* NULL is a no-op.  No work that uses it may still be pending. */
+int fr_muon_destroy(fr_muon* opt);
+
+/* The same validation on the host only, against a table instead of a plan. */
+int fr_muon_query(const fr_tensor_desc* table, uint32_t n_entries, uint64_t chunk_bytes, uint64_t arena_bytes,
+                  const fr_muon_tensor* tensors, uint32_t n, uint32_t n_groups, uint64_t grad_arena_bytes,
+                  uint64_t update_arena_bytes, const fr_muon_coeffs* coeffs, uint32_t n_steps,
+                  fr_muon_info* info);
+
+/* A state arena laid out for matrices: per matrix [param bf16 (derived from the
+ * next), master, m], contiguous and 16-aligned, src and dst offsets equal, behind
+ * what is there already: entries count from first_entry on (so that the table
+ * can be appended to one of fr_adamw_state_table), offsets from *arena_bytes and
+ * gradients of grad_dtype from *grad_bytes on, which are raised (rounded up to 16
+ * first); updates from 0 on.  Host only.
+ *   shapes   2 n numbers: rows and columns
+ * tensors (NULL or n) gets the descriptors, group 0, scale 0.2 sqrt(max(rows,
+ * cols)).  With table == NULL only the sizes are set; FR_E_RANGE if cap <
+ * *n_entries = 3 n, and where fr_muon_create refuses a shape. */
+int fr_muon_state_table(const uint32_t* shapes, uint32_t n, uint32_t grad_dtype, uint32_t first_entry,
+                        fr_tensor_desc* table, uint32_t cap, uint32_t* n_entries, fr_muon_tensor* tensors,
+                        uint64_t* arena_bytes, uint64_t* grad_bytes, uint64_t* update_bytes);
+
+/* Conventions as for the optimizer step: checked, then enqueued (kernel launches
+ * only, so all of it may be captured); calls on one optimizer share its scratch
+ * and must not overlap in time.  Buffers that a call reads or writes must not
+ * overlap.  `sums` as in fr_adamw_step; a call writes those of the entries that
+ * it writes.  stats: NULL (scale 1), or with nonfinite set a call changes
+ * neither state nor updates (sums are those of the state as it is). */
+
+/* Momenta of the state and updates <- the next ones.
+ *   state    device, 16-byte aligned, the plan's src_arena_bytes
+ *   grads    device, 16-byte aligned, grad_arena_bytes long
+ *   hyper    device, 16-byte aligned, n_groups rows
+ *   updates  device, 16-byte aligned, update_arena_bytes long; bytes outside the
+ *            matrices are not written */
+int fr_muon_direction(const fr_muon* opt, void* state, const void* grads, const fr_muon_hyper* hyper,
+                      const fr_grad_stats* stats, void* updates, fr_chunk_sum* sums, hipStream_t stream);
+
+/* updates <- the gradient arena's matrices, orthogonalised as they are (of the
+ * hyperparameters only eps is read). */
+int fr_muon_orthogonalize(const fr_muon* opt, const void* grads, const fr_muon_hyper* hyper, void* updates,
+                          hipStream_t stream);
+
+/* Masters and parameters <- the step along the updates.  (Where ranks share the
+ * orthogonalisation between them, the updates are what they exchange.) */
+int fr_muon_apply(const fr_muon* opt, void* state, const void* updates, const fr_muon_hyper* hyper,
+                  const fr_grad_stats* stats, fr_chunk_sum* sums, hipStream_t stream);
+
+/* -------------------------------------------------------------- embedding */
+
+/* The rows of an embedding that lies in the state (its bf16 parameter or its
+ * master), for a batch of tokens, and the gradient that they leave in the
+ * gradient arena, where fr_grad_norm and fr_adamw_step find it.
+ *
+ * Definitions
+ *   The table is an entry of rows x cols elements; row v belongs to token
+ *     first + v.  All other ids (those of another rank's share of the
+ *     vocabulary, negative ones, padding) belong to no row.
+ *   Lookup.  out[t] = scale * row(id_t), one fp32 product rounded to the type of
+ *     out; zeros for an id without a row.
+ *   Gradient.  g_v = scale * (the sum of dout[t] over the t with id_t = first + v),
+ *     in fp32: in ascending t in runs of FR_EMBED_RUN tokens, each summed up in
+ *     turn; the runs' sums in groups of FR_EMBED_RUN runs, each summed up in turn;
+ *     the groups' sums in turn.  grad[v] <- g_v rounded to the
+ *     gradient's type, zeros for a row without tokens; or with add, grad[v] +
+ *     g_v (one fp32 sum) rounded, rows without tokens left as they are.  Replays
+ *     and replicas get the same bits. */
+#define FR_EMBED_RUN 64
+
+/* Where an embedding is.  48 bytes, no padding. */
+typedef struct fr_embed_desc {
+  uint64_t grad_offset; /* from the gradient arena base; multiple of 16 */
+  int64_t first;        /* the token of row 0 */
+  uint64_t max_tokens;  /* of a gradient call (0: lookups only); below 2^30 */
+  uint32_t rows, cols;  /* rows * cols is the entry's numel, below 2^40 */
+  int32_t entry;        /* of the plan's table, either type */
+  uint32_t grad_dtype;  /* FR_F32 or FR_BF16 */
+  uint32_t reserved[2]; /* 0 */
+} fr_embed_desc;
+
+typedef struct fr_embed fr_embed; /* opaque, owned by the library */
+
+typedef struct fr_embed_info {
+  uint64_t rows, cols, max_tokens;
+  uint64_t arena_bytes;      /* of the state: the plan's src_arena_bytes */
+  uint64_t grad_arena_bytes;
+  uint64_t device_bytes;     /* scratch of gradient calls (0 for a query) */
+  int64_t first;
+  int64_t device;            /* -1 for a query */
+  uint32_t dtype, grad_dtype;
+} fr_embed_info;
+
+/* FR_E_INVAL: an entry outside the table, rows * cols other than its numel,
+ * rows or cols 0, a wrong dtype; FR_E_ALIGN: a gradient offset not a multiple of
+ * 16; FR_E_RANGE: a gradient past its arena, and where rows (or max_tokens / 32)
+ * times the slices of 512 columns come to 2^26.
+ * Synchronous; outside graph capture. */
+int fr_embed_create(const fr_plan* plan, const fr_embed_desc* desc, uint64_t grad_arena_bytes, fr_embed** out);
+int fr_embed_get_info(const fr_embed* e, fr_embed_info* out);
+int fr_embed_destroy(fr_embed* e);
+int fr_embed_query(const fr_tensor_desc* table, uint32_t n_entries, uint64_t arena_bytes, const fr_embed_desc* desc,
+                   uint64_t grad_arena_bytes, fr_embed_info* info);
+
+/* Checked, then enqueued; may be captured.  Gradient calls on one embedding share
+ * its scratch and must not overlap in time; lookups may.
+ *   state     device, 16-byte aligned, the plan's src_arena_bytes
+ *   ids       device, n_tokens integers of id_bytes (4 or 8, signed)
+ *   out       device, row t from element t * out_stride on (out_stride >= cols),
+ *             of out_dtype, aligned to an element */
+int fr_embed_lookup(const fr_embed* e, const void* state, const void* ids, uint32_t id_bytes, uint64_t n_tokens,
+                    float scale, void* out, uint32_t out_dtype, uint64_t out_stride, hipStream_t stream);
+/* The same of dout.
+ *   grads     device, 16-byte aligned, grad_arena_bytes long; only the
+ *             embedding's gradient is written
+ *   add       0 or 1 */
+int fr_embed_grad(const fr_embed* e, const void* ids, uint32_t id_bytes, uint64_t n_tokens, const void* dout,
+                  uint32_t dout_dtype, uint64_t dout_stride, float scale, void* grads, uint32_t add,
+                  hipStream_t stream);
+
 /* ------------------------------------------------- step tags and donors */
 
 /* Host-only controller logic that decides *which* state a restore copies and

@@ -130,6 +130,8 @@ static_assert(kSumShape[0].tile() * 4 <= FR_ADAMW_MIN_SUM_CHUNK && kSumShape[1].
 // Kernel launchers (adamw.hip): validated arguments, enqueue on `stream`,
 // return the hipError_t as an int.
 int launch_adamw_step(const AdamwStepArgs& a, void* stream);
+// The sums of a.folds and a.scales alone, chunks of up to `tiles` tiles.
+int launch_adamw_fold(const AdamwStepArgs& a, uint64_t tiles, void* stream);
 int launch_adamw_norm(const AdamwNormArgs& a, void* stream);
 int launch_adamw_scale(float max_norm, fr_grad_stats* stats, void* stream);
 int launch_adamw_convert(const AdamwConvertArgs& a, void* stream);

@@ -49,19 +49,15 @@
 
 #include "adamw.h"
 #include "device.h"
+#include "elements.h"
 
 #pragma clang fp contract(off)
 
 namespace fr {
 namespace {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
 constexpr int kDrop1 = 20, kDrop2 = 19;  // bits below a code of a first moment, of a root
 constexpr int kLift = 112;               // codes at those bits stand for 2^-112 of their magnitudes
-
-__device__ __forceinline__ float as_f(uint32_t u) { return __builtin_bit_cast(float, u); }
-__device__ __forceinline__ uint32_t as_u(float f) { return __builtin_bit_cast(uint32_t, f); }
 
 struct Tile {
   AdamwRec r;
@@ -92,58 +88,6 @@ __device__ __forceinline__ Tile tile_of(const AdamwWalk& w, const AdamwRec* recs
   t.n = j < whole ? uint32_t(T) : uint32_t(t.r.numel) % T;
   t.place = uint32_t(at);
   return t;
-}
-
-// Elements i ... i + 3 of the n > 0 at p, zeros behind them; kFull: all four are
-// there.  Else each comes by a load of its own, from the last one's place where
-// there is none: without branches all loads are in flight together.  (A load
-// within a branch is waited for before the branch ends: a step of 20,000
-// tensors of 1 to 4,096 elements took 81 us instead of 62.)
-template <bool kFull>
-__device__ __forceinline__ u32x4 load4(const void* p, uint32_t i, uint32_t n) {
-  const uint32_t* q = static_cast<const uint32_t*>(p);
-  if constexpr (kFull) return ld_nt(reinterpret_cast<const u32x4*>(q + i));
-  u32x4 x;
-#pragma unroll
-  for (uint32_t j = 0; j < 4; j++) x[j] = q[i + j < n ? i + j : n - 1];
-#pragma unroll
-  for (uint32_t j = 0; j < 4; j++) x[j] = i + j < n ? x[j] : 0u;
-  return x;
-}
-// The same of bf16 elements, in the first two words.
-template <bool kFull>
-__device__ __forceinline__ u32x4 load4h(const void* p, uint32_t i, uint32_t n) {
-  const uint16_t* q = static_cast<const uint16_t*>(p);
-  u32x4 x = {0, 0, 0, 0};
-  if constexpr (kFull) {
-    x.xy = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(q + i));
-    return x;
-  }
-  uint32_t h[4];
-#pragma unroll
-  for (uint32_t j = 0; j < 4; j++) h[j] = q[i + j < n ? i + j : n - 1];
-#pragma unroll
-  for (uint32_t j = 0; j < 4; j++) h[j] = i + j < n ? h[j] : 0u;
-  x.xy = u32x2{h[0] | h[1] << 16, h[2] | h[3] << 16};
-  return x;
-}
-// Their fp32 patterns.
-__device__ __forceinline__ u32x4 widen(const u32x4& x) {
-  return u32x4{x.x << 16, x.x & 0xFFFF0000u, x.y << 16, x.y & 0xFFFF0000u};
-}
-template <bool kFull>
-__device__ __forceinline__ void store4(void* p, u32x4 x, uint32_t i, uint32_t n) {
-  uint32_t* q = static_cast<uint32_t*>(p) + i;
-  if (kFull || i + 4 <= n) return st_nt(x, reinterpret_cast<u32x4*>(q));
-  for (int j = 0; j < 4; j++)
-    if (i + j < n) q[j] = x[j];
-}
-template <bool kFull>
-__device__ __forceinline__ void store4h(void* p, u32x2 x, uint32_t i, uint32_t n) {
-  uint16_t* q = static_cast<uint16_t*>(p) + i;
-  if (kFull || i + 4 <= n) return st_nt2(x, reinterpret_cast<u32x2*>(q));
-  for (int j = 0; j < 4; j++)
-    if (i + j < n) q[j] = uint16_t(x[j / 2] >> (16 * (j & 1)));
 }
 
 // ------------------------------------------------------------ 8-bit moments
@@ -294,14 +238,6 @@ __device__ __forceinline__ void encode4(const f32x4& m, const f32x4& r, uint64_t
   *cr = pack_top(b) & (xr.bad ? 0u : ~0u);
   *sm = xm.scale;
   *sr = xr.scale;
-}
-
-// Four fp32 patterns to bf16, two a word: v_cvt_pk_bf16_f32 rounds every
-// pattern as rne_bf16 does, NaNs included.
-__device__ __forceinline__ u32x2 to_bf16(const f32x4& x) {
-  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-  return u32x2{__builtin_bit_cast(uint32_t, __builtin_convertvector(x.xy, bf16x2)),
-               __builtin_bit_cast(uint32_t, __builtin_convertvector(x.zw, bf16x2))};
 }
 
 // ------------------------------------------------ square roots and quotients
@@ -873,15 +809,7 @@ int step(const AdamwStepArgs& a, hipStream_t st) {
   const int e = int(hipGetLastError());
   if (e != 0 || !kSums || a.n_folds == 0) return e;
   // tiles of the longest chunks that are fed by tiles: parameters', or codes'
-  const uint64_t tiles = a.C / (kEight ? 1 : 2) / s.tile();
-  const auto fold = [&](auto kernel, uint32_t lanes) {
-    const uint32_t per = 256 / lanes;
-    hipLaunchKernelGGL(kernel, dim3(a.n_scales + (a.n_folds + per - 1) / per), dim3(256), 0, st, a.folds, a.n_folds,
-                       a.scales, a.n_scales, a.walk.stride, a.parts, static_cast<const uint8_t*>(a.state), a.sums);
-  };
-  if (tiles >= 256) fold(k_adamw_fold<64>, 64);
-  else fold(k_adamw_fold<16>, 16);
-  return int(hipGetLastError());
+  return launch_adamw_fold(a, a.C / (kEight ? 1 : 2) / s.tile(), st);
 }
 
 template <bool kEight>
@@ -898,6 +826,18 @@ int launch_adamw_step(const AdamwStepArgs& a, void* stream) {
   const hipStream_t st = hipStream_t(stream);
   if (a.parts) return a.eight ? step<true, true>(a, st) : step<false, true>(a, st);
   return a.eight ? step<true, false>(a, st) : step<false, false>(a, st);
+}
+
+int launch_adamw_fold(const AdamwStepArgs& a, uint64_t tiles, void* stream) {
+  const auto fold = [&](auto kernel, uint32_t lanes) {
+    const uint32_t per = 256 / lanes;
+    hipLaunchKernelGGL(kernel, dim3(a.n_scales + (a.n_folds + per - 1) / per), dim3(256), 0, hipStream_t(stream),
+                       a.folds, a.n_folds, a.scales, a.n_scales, a.walk.stride, a.parts,
+                       static_cast<const uint8_t*>(a.state), a.sums);
+  };
+  if (tiles >= 256) fold(k_adamw_fold<64>, 64);
+  else fold(k_adamw_fold<16>, 16);
+  return int(hipGetLastError());
 }
 
 int launch_adamw_norm(const AdamwNormArgs& a, void* stream) {

@@ -48,6 +48,17 @@ HYPER_DTYPE = np.dtype(
      ("bias2", "<f4"), ("seed", "<u4")]
 )
 STATS_BYTES = 24  # fr_grad_stats
+# fr_muon_tensor: 56 bytes.
+MUON_DTYPE = np.dtype(
+    [("grad_offset", "<u8"), ("update_offset", "<u8"), ("rows", "<u4"), ("cols", "<u4"), ("grad_dtype", "<u4"),
+     ("group", "<u4"), ("param", "<i4"), ("master", "<i4"), ("m", "<i4"), ("flags", "<u4"), ("scale", "<f4"),
+     ("reserved", "<u4")]
+)
+# fr_muon_hyper: 32 bytes.
+MUON_HYPER_DTYPE = np.dtype(
+    [("lr", "<f4"), ("momentum", "<f4"), ("eps", "<f4"), ("weight_decay", "<f4"), ("nesterov", "<u4"),
+     ("reserved", "<u4", 3)]
+)
 FR_ADAMW_BLOCK = 256
 FR_ADAMW_SPAN = 1024
 FR_ADAMW_MIN_SUM_CHUNK = 4096
@@ -83,6 +94,29 @@ class fr_adamw_info(C.Structure):
     _fields_ = [(f, C.c_uint64) for f in ("n_tensors", "n_groups", "n_elements", "n_elements_8bit", "n_counters",
                                           "grad_arena_bytes", "arena_bytes", "sums_chunks",
                                           "device_bytes")] + [("device", C.c_int64)]
+
+    def as_dict(self):
+        return {f: getattr(self, f) for f, _ in self._fields_}
+
+
+class fr_muon_info(C.Structure):
+    _fields_ = [(f, C.c_uint64) for f in ("n_tensors", "n_groups", "n_steps", "n_elements", "multiplications",
+                                          "grad_arena_bytes", "update_arena_bytes", "arena_bytes", "sums_chunks",
+                                          "device_bytes")] + [("device", C.c_int64)]
+
+    def as_dict(self):
+        return {f: getattr(self, f) for f, _ in self._fields_}
+
+
+class fr_embed_desc(C.Structure):
+    _fields_ = [("grad_offset", C.c_uint64), ("first", C.c_int64), ("max_tokens", C.c_uint64), ("rows", C.c_uint32),
+                ("cols", C.c_uint32), ("entry", C.c_int32), ("grad_dtype", C.c_uint32), ("reserved", C.c_uint32 * 2)]
+
+
+class fr_embed_info(C.Structure):
+    _fields_ = [(f, C.c_uint64) for f in ("rows", "cols", "max_tokens", "arena_bytes", "grad_arena_bytes",
+                                          "device_bytes")] + [
+        ("first", C.c_int64), ("device", C.c_int64), ("dtype", C.c_uint32), ("grad_dtype", C.c_uint32)]
 
     def as_dict(self):
         return {f: getattr(self, f) for f, _ in self._fields_}
@@ -152,6 +186,21 @@ def _load():
         "fr_grad_scale": [P, C.c_float, P, P],
         "fr_adamw_step": [P, P, P, P, P, P, P],
         "fr_adamw_convert": [P, P, P, P, u32, P],
+        "fr_muon_create": [P, P, u32, u32, u64, u64, P, u32, C.POINTER(P)],
+        "fr_muon_get_info": [P, C.POINTER(fr_muon_info)],
+        "fr_muon_destroy": [P],
+        "fr_muon_query": [P, u32, u64, u64, P, u32, u32, u64, u64, P, u32, C.POINTER(fr_muon_info)],
+        "fr_muon_state_table": [P, u32, u32, u32, P, u32, C.POINTER(u32), P, C.POINTER(u64), C.POINTER(u64),
+                                C.POINTER(u64)],
+        "fr_muon_direction": [P, P, P, P, P, P, P, P],
+        "fr_muon_orthogonalize": [P, P, P, P, P],
+        "fr_muon_apply": [P, P, P, P, P, P, P],
+        "fr_embed_create": [P, P, u64, C.POINTER(P)],
+        "fr_embed_get_info": [P, C.POINTER(fr_embed_info)],
+        "fr_embed_destroy": [P],
+        "fr_embed_query": [P, u32, u64, P, u64, C.POINTER(fr_embed_info)],
+        "fr_embed_lookup": [P, P, P, u32, u64, C.c_float, P, u32, u64, P],
+        "fr_embed_grad": [P, P, u32, u64, P, u32, u64, C.c_float, P, u32, P],
         "fr_tracker_create": [u32, P, C.c_double, C.c_double, C.POINTER(P)],
         "fr_tracker_destroy": [P],
         "fr_tracker_heartbeat": [P, u32, C.c_int64, C.c_double],
@@ -186,6 +235,9 @@ EXPORTED = (
     "fr_pack_chunks", "fr_unpack_chunks", "fr_pack_flagged", "fr_unpack_flagged",
     "fr_adamw_create", "fr_adamw_get_info", "fr_adamw_destroy", "fr_adamw_query", "fr_adamw_state_table",
     "fr_grad_norm", "fr_grad_scale", "fr_adamw_step", "fr_adamw_convert",
+    "fr_muon_create", "fr_muon_get_info", "fr_muon_destroy", "fr_muon_query", "fr_muon_state_table",
+    "fr_muon_direction", "fr_muon_orthogonalize", "fr_muon_apply",
+    "fr_embed_create", "fr_embed_get_info", "fr_embed_destroy", "fr_embed_query", "fr_embed_lookup", "fr_embed_grad",
     "fr_tracker_create", "fr_tracker_destroy", "fr_tracker_heartbeat",
     "fr_tracker_report_failure", "fr_tracker_decide", "fr_tracker_failed_ranks", "fr_tracker_donors",
     "fr_layout_rank_coords", "fr_layout_donors", "fr_layout_state_table",
@@ -700,6 +752,284 @@ def fr_adamw_convert(from_opt: AdamW, from_state, to_opt: AdamW, to_state, seed:
     _check(_lib.fr_adamw_convert(from_opt.handle, _dev(from_state, from_opt.info["arena_bytes"], "from_state"),
                                  to_opt.handle, _dev(to_state, to_opt.info["arena_bytes"], "to_state"), seed,
                                  _stream(stream)), "fr_adamw_convert")
+
+
+def muon_hyper(groups) -> np.ndarray:
+    """A fr_muon_hyper array: a dict for each group, with lr and, where they
+    differ from these, momentum 0.95, nesterov True, eps 1e-7, weight_decay 0."""
+    h = np.zeros(len(groups), MUON_HYPER_DTYPE)
+    for row, g in zip(h, groups):
+        unknown = set(g) - {"lr", "momentum", "eps", "weight_decay", "nesterov"}
+        if unknown:
+            raise ValueError(f"unknown hyperparameters: {sorted(unknown)}")
+        row["lr"], row["momentum"], row["eps"] = g["lr"], g.get("momentum", 0.95), g.get("eps", 1e-7)
+        row["weight_decay"], row["nesterov"] = g.get("weight_decay", 0.0), bool(g.get("nesterov", True))
+    return h
+
+
+def _muon_rows(tensors) -> np.ndarray:
+    """A contiguous fr_muon_tensor array (any structured array with these
+    fields, or rows in their order)."""
+    if isinstance(tensors, np.ndarray) and tensors.dtype.names:
+        out = np.zeros(len(tensors), dtype=MUON_DTYPE)
+        for f in tensors.dtype.names:
+            out[f] = tensors[f]
+        return out
+    return np.array([tuple(r) for r in tensors], dtype=MUON_DTYPE)
+
+
+def _coeffs(coeffs):
+    """A contiguous array of (a, b, c) steps; None: the library's."""
+    if coeffs is None:
+        return None, 0
+    c = np.ascontiguousarray(coeffs, np.float32)
+    if c.ndim != 2 or c.shape[1] != 3:
+        raise ValueError("coeffs: (a, b, c) for each step")
+    return c, len(c)
+
+
+def fr_muon_query(table, chunk_bytes: int, arena_bytes: int, tensors, n_groups: int, grad_arena_bytes: int,
+                  update_arena_bytes: int, coeffs=None) -> dict:
+    """Host-only validation of an optimizer against a table: its info."""
+    t, r, (c, n) = as_table(table), _muon_rows(tensors), _coeffs(coeffs)
+    info = fr_muon_info()
+    _check(_lib.fr_muon_query(t.ctypes.data if len(t) else None, len(t), chunk_bytes, arena_bytes,
+                              r.ctypes.data if len(r) else None, len(r), n_groups, grad_arena_bytes,
+                              update_arena_bytes, None if c is None else c.ctypes.data, n, C.byref(info)),
+           "fr_muon_query")
+    return info.as_dict()
+
+
+def fr_muon_state_table(shapes, grad_dtype: int = FR_BF16, first_entry: int = 0, arena_bytes: int = 0,
+                        grad_bytes: int = 0):
+    """(table, tensors, arena bytes, gradient arena bytes, update arena bytes)
+    of matrices of these (rows, cols), behind first_entry entries and so many
+    bytes of state and gradients (those of fr_adamw_state_table, to whose table
+    this one is then appended)."""
+    s = np.asarray(shapes)
+    if s.size and (s.ndim != 2 or s.shape[1] != 2):
+        raise ValueError("shapes: (rows, cols) for each matrix")
+    if s.size and (s.min() < 0 or s.max() > 0xFFFFFFFF):
+        raise ValueError("shapes: rows and cols are 32-bit counts")
+    s = np.ascontiguousarray(s, np.uint32)
+    n = len(s) if s.size else 0
+    ne, ab, gb, ub = C.c_uint32(), C.c_uint64(arena_bytes), C.c_uint64(grad_bytes), C.c_uint64()
+    r, t = np.zeros(n, MUON_DTYPE), np.zeros(3 * n, DESC_DTYPE)
+    _check(_lib.fr_muon_state_table(s.ctypes.data if n else None, n, grad_dtype, first_entry,
+                                    t.ctypes.data if n else None, t.size, C.byref(ne), r.ctypes.data if n else None,
+                                    C.byref(ab), C.byref(gb), C.byref(ub)), "fr_muon_state_table")
+    return t, r, ab.value, gb.value, ub.value
+
+
+class Muon:
+    """The step by orthogonalised momentum over matrices of a plan's table
+    (``fr_muon_*``), bound to the plan's device.  Its calls share scratch memory
+    and must not overlap in time: those on several streams have to wait for
+    each other."""
+
+    def __init__(self, plan: Plan, tensors, n_groups: int, grad_arena_bytes: int, update_arena_bytes: int,
+                 coeffs=None):
+        self._h = None
+        r, (c, n) = _muon_rows(tensors), _coeffs(coeffs)
+        h = C.c_void_p()
+        _check(_lib.fr_muon_create(plan.handle, r.ctypes.data if len(r) else None, len(r), n_groups, grad_arena_bytes,
+                                   update_arena_bytes, None if c is None else c.ctypes.data, n, C.byref(h)),
+               "fr_muon_create")
+        self._h = h
+        info = fr_muon_info()
+        _check(_lib.fr_muon_get_info(self._h, C.byref(info)), "fr_muon_get_info")
+        self.info = info.as_dict()
+        self.n_chunks = plan.n_chunks
+
+    @property
+    def handle(self):
+        if self._h is None:
+            raise ValueError("optimizer destroyed")
+        return self._h
+
+    def destroy(self):
+        if self._h is not None:
+            _lib.fr_muon_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+    def empty_updates(self, device="cuda"):
+        import torch
+
+        return torch.empty(max(self.info["update_arena_bytes"], 16), dtype=torch.uint8, device=device)
+
+    def direction(self, state, grads, hyper, updates, stats=None, sums=None, stream=None):
+        return fr_muon_direction(self, state, grads, hyper, updates, stats, sums, stream)
+
+    def orthogonalize(self, grads, hyper, updates, stream=None):
+        return fr_muon_orthogonalize(self, grads, hyper, updates, stream)
+
+    def apply(self, state, updates, hyper, stats=None, sums=None, stream=None):
+        return fr_muon_apply(self, state, updates, hyper, stats, sums, stream)
+
+
+def fr_muon_create(plan: Plan, tensors, n_groups: int, grad_arena_bytes: int, update_arena_bytes: int,
+                   coeffs=None) -> Muon:
+    return Muon(plan, tensors, n_groups, grad_arena_bytes, update_arena_bytes, coeffs)
+
+
+def fr_muon_destroy(opt: Muon) -> None:
+    opt.destroy()
+
+
+def fr_muon_direction(opt: Muon, state, grads, hyper, updates, stats=None, sums=None, stream=None) -> None:
+    """hyper: a device tensor of n_groups rows of 32 bytes (a muon_hyper array
+    copied there); stats None: gradients as they are; sums None: none."""
+    i = opt.info
+    _check(_lib.fr_muon_direction(opt.handle, _dev(state, i["arena_bytes"], "state"),
+                                  _dev(grads, i["grad_arena_bytes"], "grads"),
+                                  _dev(hyper, MUON_HYPER_DTYPE.itemsize * i["n_groups"], "hyper"),
+                                  _dev(stats, STATS_BYTES, "stats"), _dev(updates, i["update_arena_bytes"], "updates"),
+                                  _dev(sums, SUM_BYTES * opt.n_chunks, "sums"), _stream(stream)), "fr_muon_direction")
+
+
+def fr_muon_orthogonalize(opt: Muon, grads, hyper, updates, stream=None) -> None:
+    i = opt.info
+    _check(_lib.fr_muon_orthogonalize(opt.handle, _dev(grads, i["grad_arena_bytes"], "grads"),
+                                      _dev(hyper, MUON_HYPER_DTYPE.itemsize * i["n_groups"], "hyper"),
+                                      _dev(updates, i["update_arena_bytes"], "updates"), _stream(stream)),
+           "fr_muon_orthogonalize")
+
+
+def fr_muon_apply(opt: Muon, state, updates, hyper, stats=None, sums=None, stream=None) -> None:
+    i = opt.info
+    _check(_lib.fr_muon_apply(opt.handle, _dev(state, i["arena_bytes"], "state"),
+                              _dev(updates, i["update_arena_bytes"], "updates"),
+                              _dev(hyper, MUON_HYPER_DTYPE.itemsize * i["n_groups"], "hyper"),
+                              _dev(stats, STATS_BYTES, "stats"), _dev(sums, SUM_BYTES * opt.n_chunks, "sums"),
+                              _stream(stream)), "fr_muon_apply")
+
+
+def _rows2d(x, n: int, cols: int, name: str):
+    """(address, dtype, elements from row to row) of a device tensor of n rows of
+    cols bf16 or fp32 elements, the elements of a row next to each other."""
+    import torch
+
+    if not x.is_cuda:
+        raise ValueError(f"{name}: not a device tensor")
+    if x.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"{name}: {x.dtype}, not float32 or bfloat16")
+    if x.dim() < 2 or x.shape[-1] != cols or x.numel() != n * cols:
+        raise ValueError(f"{name}: shape {tuple(x.shape)} for {n} rows of {cols}")
+    if n and x.dim() > 2:
+        try:
+            x = x.view(n, cols)
+        except RuntimeError:
+            raise ValueError(f"{name}: its rows are not evenly spaced") from None
+    stride = cols
+    if n:
+        if cols > 1 and x.stride(1) != 1:
+            raise ValueError(f"{name}: a row's elements are not next to each other")
+        if n > 1:
+            stride = x.stride(0)
+            if stride < cols:
+                raise ValueError(f"{name}: rows overlap")
+    return x.data_ptr() or None, FR_F32 if x.dtype == torch.float32 else FR_BF16, stride
+
+
+def _ids_of(ids):
+    """(address, bytes of one, how many) of a device tensor of tokens."""
+    import torch
+
+    if not ids.is_cuda:
+        raise ValueError("ids: not a device tensor")
+    if ids.dtype not in (torch.int32, torch.int64):
+        raise ValueError(f"ids: {ids.dtype}, not int32 or int64")
+    if not ids.is_contiguous():
+        raise ValueError("ids: not contiguous")
+    return ids.data_ptr() or None, ids.element_size(), ids.numel()
+
+
+class Embedding:
+    """An embedding that lies in a plan's state (``fr_embed_*``): entry `entry`
+    of its table, rows x cols, row 0 for token `first`; its gradient from
+    grad_offset on in a gradient arena.  max_tokens 0: lookups only.  Gradient
+    calls share scratch memory and must not overlap in time."""
+
+    def __init__(self, plan: Plan, entry: int, rows: int, cols: int, max_tokens: int = 0, first: int = 0,
+                 grad_dtype: int = FR_BF16, grad_arena_bytes: int = 0, grad_offset: int = 0):
+        self._h = None
+        h = C.c_void_p()
+        d = _embed_desc(entry, rows, cols, max_tokens, first, grad_dtype, grad_offset)
+        _check(_lib.fr_embed_create(plan.handle, C.byref(d), grad_arena_bytes, C.byref(h)), "fr_embed_create")
+        self._h = h
+        info = fr_embed_info()
+        _check(_lib.fr_embed_get_info(self._h, C.byref(info)), "fr_embed_get_info")
+        self.info = info.as_dict()
+
+    handle = Muon.handle
+
+    def destroy(self):
+        if self._h is not None:
+            _lib.fr_embed_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+    def lookup(self, state, ids, out, scale=1.0, stream=None):
+        return fr_embed_lookup(self, state, ids, out, scale, stream)
+
+    def grad(self, ids, dout, grads, scale=1.0, add=False, stream=None):
+        return fr_embed_grad(self, ids, dout, grads, scale, add, stream)
+
+
+def _embed_desc(entry, rows, cols, max_tokens, first, grad_dtype, grad_offset):
+    for name, x, top in (("rows", rows, 1 << 32), ("cols", cols, 1 << 32), ("max_tokens", max_tokens, 1 << 64),
+                         ("grad_offset", grad_offset, 1 << 64)):
+        if not 0 <= x < top:
+            raise ValueError(f"{name}: {x}")
+    return fr_embed_desc(grad_offset, first, max_tokens, rows, cols, entry, grad_dtype)
+
+
+def fr_embed_query(table, arena_bytes: int, entry: int, rows: int, cols: int, max_tokens: int = 0, first: int = 0,
+                   grad_dtype: int = FR_BF16, grad_arena_bytes: int = 0, grad_offset: int = 0) -> dict:
+    """Host-only validation of an embedding against a table: its info."""
+    t, info = as_table(table), fr_embed_info()
+    d = _embed_desc(entry, rows, cols, max_tokens, first, grad_dtype, grad_offset)
+    _check(_lib.fr_embed_query(t.ctypes.data if len(t) else None, len(t), arena_bytes, C.byref(d), grad_arena_bytes,
+                               C.byref(info)), "fr_embed_query")
+    return info.as_dict()
+
+
+def fr_embed_create(plan: Plan, entry: int, rows: int, cols: int, **more) -> Embedding:
+    return Embedding(plan, entry, rows, cols, **more)
+
+
+def fr_embed_destroy(e: Embedding) -> None:
+    e.destroy()
+
+
+def fr_embed_lookup(e: Embedding, state, ids, out, scale: float = 1.0, stream=None) -> None:
+    """out (of ids' shape and a last dimension of cols, bf16 or fp32; rows may be
+    further apart than cols) <- scale * the rows of ids (int32 or int64)."""
+    p, size, n = _ids_of(ids)
+    q, dtype, stride = _rows2d(out, n, e.info["cols"], "out")
+    _check(_lib.fr_embed_lookup(e.handle, _dev(state, e.info["arena_bytes"], "state"), p, size, n, scale, q, dtype,
+                                stride, _stream(stream)), "fr_embed_lookup")
+
+
+def fr_embed_grad(e: Embedding, ids, dout, grads, scale: float = 1.0, add: bool = False, stream=None) -> None:
+    """The embedding's gradient in the arena `grads` <- (add: += ) that of dout,
+    which is as `out` of a lookup."""
+    p, size, n = _ids_of(ids)
+    q, dtype, stride = _rows2d(dout, n, e.info["cols"], "dout")
+    _check(_lib.fr_embed_grad(e.handle, p, size, n, q, dtype, stride, scale,
+                              _dev(grads, e.info["grad_arena_bytes"], "grads"), int(bool(add)), _stream(stream)),
+           "fr_embed_grad")
 
 
 class Tracker:
