@@ -39,6 +39,7 @@ struct MuonLayout {
   // first chunks, and how many, of each matrix's param, master and momentum
   std::vector<uint32_t> chunk0, n_chunks;
   std::vector<fr_muon_coeffs> coeffs;
+  uint32_t side = kMuonSmall;
   uint64_t scratch = 0;  // bytes
   fr_muon_info info{};
 };
@@ -75,6 +76,30 @@ int check_coeffs(const fr_muon_coeffs* c, uint32_t n, std::vector<fr_muon_coeffs
     }
   }
   return FR_OK;
+}
+
+// Which tiles the products take, and where in the scratch their operands lie.
+void lay_out_scratch(MuonLayout* out) {
+  uint64_t large = 0;
+  for (const MuonRec& r : out->recs) {
+    const uint64_t m = (r.m + kMuonLarge - 1) / kMuonLarge, n = (r.n + kMuonLarge - 1) / kMuonLarge;
+    large += r.numel ? m * n : 0;
+  }
+  out->side = large >= 256 ? kMuonLarge : kMuonSmall;
+  for (MuonRec& r : out->recs) {
+    r.mp = uint32_t(up(r.m, out->side));
+    r.np = uint32_t(up(r.n, out->side));
+    if (!r.numel) continue;
+    const uint64_t wide = uint64_t(r.mp) * r.np, square = uint64_t(r.mp) * r.mp;
+    const struct {
+      uint64_t* where;
+      uint64_t bytes;
+    } parts[5] = {{&r.x[0], 2 * wide}, {&r.x[1], 2 * wide}, {&r.rest, wide}, {&r.a, 2 * square}, {&r.q, 2 * square}};
+    for (const auto& p : parts) {
+      *p.where = out->scratch;
+      out->scratch += p.bytes;
+    }
+  }
 }
 
 int validate(const fr_tensor_desc* table, uint32_t n_entries, const Layout& L, uint64_t arena_bytes,
@@ -145,8 +170,6 @@ int validate(const fr_tensor_desc* table, uint32_t n_entries, const Layout& L, u
     r.wide = d.rows <= d.cols;
     r.m = std::min(d.rows, d.cols);
     r.n = std::max(d.rows, d.cols);
-    r.mp = uint32_t(up(r.m, kMuonSide));
-    r.np = uint32_t(up(r.n, kMuonSide));
     // entries of X_0 are some 1 / sqrt(m n), of an orthogonal matrix 1 / sqrt(n)
     r.lift = float(std::ldexp(1.0, int(std::lround(0.5 * std::log2(double(std::max(r.n, 1u)))))));
     info.n_elements += numel;
@@ -154,19 +177,8 @@ int validate(const fr_tensor_desc* table, uint32_t n_entries, const Layout& L, u
     r.slot0 = tiles;
     r.slots = (numel + kMuonTile - 1) / kMuonTile;
     tiles += r.slots;
-    if (!numel) continue;
-    const uint64_t wide = uint64_t(r.mp) * r.np, square = uint64_t(r.mp) * r.mp;
-    uint64_t& at = out->scratch;
-    const struct {
-      uint64_t* where;
-      uint64_t bytes;
-    } parts[6] = {{&r.x, 2 * wide}, {&r.xt[0], 2 * wide}, {&r.xt[1], 2 * wide}, {&r.xc, 4 * wide},
-                  {&r.a, 2 * square}, {&r.q, 2 * square}};
-    for (const auto& p : parts) {
-      *p.where = at;
-      at += p.bytes;
-    }
   }
+  lay_out_scratch(out);
   if (twice) return FR_E_OVERLAP;
   if (!disjoint(written) || !disjoint(updated)) return FR_E_OVERLAP;
   if (strange) return FR_E_INVAL;
@@ -207,17 +219,24 @@ struct Carver {
 };
 
 // The tiles of a product over all matrices, those of the longest sums first, so
-// that no workgroup starts a long one last.
+// that no workgroup starts a long one last.  Workgroup b runs on die b mod 8, and
+// each die takes runs of kRun tiles in order, which share most of their operands'
+// rows, from its own L2.
 struct TileList {
+  static constexpr size_t kRun = 16;
   struct Item {
     uint64_t tile;
     uint32_t k;
   };
   std::vector<Item> items;
-  std::vector<uint64_t> sorted() {
+  std::vector<uint64_t> dealt() {
     std::stable_sort(items.begin(), items.end(), [](const Item& a, const Item& b) { return a.k > b.k; });
-    std::vector<uint64_t> d(items.size());
-    for (size_t i = 0; i < d.size(); i++) d[i] = items[i].tile;
+    const size_t n = items.size(), whole = n / (8 * kRun) * (8 * kRun);
+    std::vector<uint64_t> d(n);
+    for (size_t b = 0; b < n; b++) {
+      const size_t i = b % (8 * kRun);
+      d[b] = items[b < whole ? b - i + i % 8 * kRun + i / 8 : b].tile;
+    }
     return d;
   }
 };
@@ -226,7 +245,8 @@ int build(fr_muon* o) {
   const MuonLayout& Y = o->layout;
   const uint32_t n = uint32_t(Y.recs.size());
   std::vector<uint64_t> walk;
-  TileList gram, whole, spread;
+  std::vector<uint64_t> spread;
+  TileList gram, whole;
   std::vector<AdamwFold> mom, step;
   const bool sums = o->C >= FR_ADAMW_MIN_SUM_CHUNK;
   uint64_t slots = 0;
@@ -241,14 +261,13 @@ int build(fr_muon* o) {
       walk[(g & 7) * stride + (g >> 3)] = id | i;
     }
     if (!r.numel) continue;
-    const uint32_t tm = r.mp / kMuonSide, tn = r.np / kMuonSide;
+    const uint32_t tm = r.mp / Y.side, tn = r.np / Y.side;
     for (uint32_t i = 0; i < tm; i++)
       for (uint32_t j = 0; j <= i; j++) gram.items.push_back({id | uint64_t(i) << 16 | j, r.np});
     for (uint32_t j = 0; j < tn; j++)
-      for (uint32_t i = 0; i < tm; i++) {
-        whole.items.push_back({id | uint64_t(i) << 16 | j, r.mp});
-        spread.items.push_back({id | uint64_t(i) << 16 | j, 0});
-      }
+      for (uint32_t i = 0; i < tm; i++) whole.items.push_back({id | uint64_t(i) << 16 | j, r.mp});
+    for (uint32_t i = 0; i < r.mp / 64; i++)
+      for (uint32_t j = 0; j < r.np / 64; j++) spread.push_back(id | uint64_t(i) << 16 | j);
     if (!sums) continue;
     // chunk i of an array holds this many elements, and so these tiles
     const uint64_t per[3] = {o->C / 2, o->C / 4, o->C / 4};
@@ -260,14 +279,14 @@ int build(fr_muon* o) {
         (j == 2 ? mom : step).push_back(f);
       }
   }
-  const std::vector<uint64_t> t_gram = gram.sorted(), t_whole = whole.sorted(), t_spread = spread.sorted();
+  const std::vector<uint64_t> t_gram = gram.dealt(), t_whole = whole.dealt();
   Carver c;
   const size_t recs = c.add(Y.recs.data(), n * sizeof(MuonRec));
   const fr_grad_stats neutral = {0.0, 0.0f, 1.0f, 0};
   const size_t ns = c.add(&neutral, sizeof neutral);
   const size_t wa = c.add(walk.data(), walk.size() * 8);
   const size_t tg = c.add(t_gram.data(), t_gram.size() * 8), tw = c.add(t_whole.data(), t_whole.size() * 8);
-  const size_t ts = c.add(t_spread.data(), t_spread.size() * 8);
+  const size_t ts = c.add(spread.data(), spread.size() * 8);
   const size_t fm = c.add(mom.data(), mom.size() * sizeof(AdamwFold));
   const size_t fs = c.add(step.data(), step.size() * sizeof(AdamwFold));
   const size_t np = c.add(nullptr, 8 * stride * sizeof(double));
@@ -296,11 +315,12 @@ int build(fr_muon* o) {
   MuonArgs& a = o->args;
   a.recs = reinterpret_cast<const MuonRec*>(at(recs));
   a.n = n;
+  a.side = Y.side;
   a.walk = AdamwWalk{reinterpret_cast<const uint64_t*>(at(wa)), slots, stride};
   a.scratch = at(sc);
   a.parts = reinterpret_cast<double*>(at(np));
   a.factors = reinterpret_cast<double*>(at(nf));
-  a.spread = MuonTiles{reinterpret_cast<const uint64_t*>(at(ts)), t_spread.size()};
+  a.spread = MuonTiles{reinterpret_cast<const uint64_t*>(at(ts)), spread.size()};
   a.gram = MuonTiles{reinterpret_cast<const uint64_t*>(at(tg)), t_gram.size()};
   a.whole = MuonTiles{reinterpret_cast<const uint64_t*>(at(tw)), t_whole.size()};
   a.coeffs = Y.coeffs.data();

@@ -12,26 +12,26 @@ namespace fr {
 // One matrix, as the kernels read it (uniform loads).  m <= n are its sides, mp
 // and np the same in whole tiles.  Offsets in bytes: of the state, the arenas
 // and, for what the products read and write, the optimizer's scratch:
-//   x    mp x np, fp16    X
-//   xt   np x mp, fp16    its transpose, twice: read and written in turn
-//   xc   mp x np, fp32    X, as carried
-//   a, q mp x mp, fp16    X X^T and the polynomial of it
+//   x     mp x np, fp16    X, twice: read and written in turn
+//   rest  mp x np, 8 bits  what X is more than its fp16 number
+//   a, q  mp x mp, fp16    X X^T and the polynomial of it
 struct alignas(16) MuonRec {
   uint64_t numel;
   uint64_t grad, update, param, master, mom;  // param: kNone if it has none
-  uint64_t x, xt[2], xc, a, q;
+  uint64_t x[2], rest, a, q;
   uint64_t slot0, slots;  // its tiles in the walk over elements
   uint32_t cols, m, n, mp, np;
   uint32_t wide;      // rows <= cols: X has the matrix's own rows
   uint32_t grad_f32, group;
   float scale;
   float lift;         // the power of two that X is stored times
-  uint32_t pad_[2];
+  uint32_t pad_[4];
 };
 static_assert(sizeof(MuonRec) == 160, "MuonRec is 160 bytes");
 
 constexpr uint32_t kMuonTile = 1024;  // elements of a workgroup of the walk over elements
-constexpr uint32_t kMuonSide = 128;   // sides of matrices are padded to it
+// Sides of the products' tiles, to which those of matrices are padded.
+constexpr uint32_t kMuonLarge = 256, kMuonSmall = 64;
 constexpr float kMuonLiftA = 256.0f;  // A and Q are stored times this
 
 // A product's work: (matrix << 32) | (tile row << 16) | tile column, one for each
@@ -44,6 +44,7 @@ struct MuonTiles {
 struct MuonArgs {
   const MuonRec* recs = nullptr;
   uint32_t n = 0;
+  uint32_t side = kMuonSmall;  // of the products' tiles
   AdamwWalk walk;          // tiles of kMuonTile elements
   uint8_t* scratch = nullptr;
   double* parts = nullptr;  // a sum of squares for each place of the walk
@@ -54,7 +55,8 @@ struct MuonArgs {
   const void* grads = nullptr;
   void* updates = nullptr;
   bool momentum = false;   // of the state; else the gradients as they are
-  MuonTiles spread, gram, whole;
+  MuonTiles spread;  // tiles of 64 x 64
+  MuonTiles gram, whole;
   const fr_muon_coeffs* coeffs = nullptr;
   uint32_t n_steps = 0;
   // sums, or sum_parts == NULL

@@ -169,48 +169,119 @@ __global__ __launch_bounds__(256) void k_muon_norm(MuonArgs a) {
   }
 }
 
-// X_0 of a tile: fp32, fp16 and transposed; zeros behind the matrix's sides.
+// ------------------------------------------------------------ X, as carried
+
+// X between steps: fp16, and where the next step wants it closer the rest in 8
+// bits, in 256ths of the fp16 number's last place, of which it is half at most.
+typedef int8_t i8x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ float last_place(f16 h) {
+  const uint32_t e = __builtin_bit_cast(uint16_t, h) >> 10 & 31;
+  return as_f(((e ? e : 1) + 127 - 25) << 23);
+}
+__device__ __forceinline__ int8_t rest_of(float v, f16 h) {
+  const float q = __builtin_rintf((v - float(h)) * 256.0f / last_place(h));
+  return int8_t(__builtin_fminf(q, 127.0f));  // (NaN, of an infinity: any)
+}
+__device__ __forceinline__ float with_rest(f16 h, int8_t rest) {
+  return __builtin_fmaf(float(rest), last_place(h) * (1.0f / 256.0f), float(h));
+}
+
+// Four elements of a row of n from any element's address on, zeros behind them.
+struct __attribute__((packed, aligned(2))) Half4 {
+  uint16_t x[4];
+};
+struct __attribute__((packed, aligned(4))) Float4 {
+  float x[4];
+};
+template <bool kF32>
+__device__ __forceinline__ f32x4 load_four(const void* p, uint64_t at, uint32_t left) {
+  f32x4 v = {0, 0, 0, 0};
+  if (left >= 4) {
+    if constexpr (kF32) {
+      const Float4 f = *reinterpret_cast<const Float4*>(static_cast<const float*>(p) + at);
+#pragma unroll
+      for (int j = 0; j < 4; j++) v[j] = f.x[j];
+    } else {
+      const Half4 h = *reinterpret_cast<const Half4*>(static_cast<const uint16_t*>(p) + at);
+#pragma unroll
+      for (int j = 0; j < 4; j++) v[j] = as_f(uint32_t(h.x[j]) << 16);
+    }
+    return v;
+  }
+#pragma unroll
+  for (uint32_t j = 0; j < 4; j++)
+    if (j < left)
+      v[j] = kF32 ? static_cast<const float*>(p)[at + j]
+                  : as_f(uint32_t(static_cast<const uint16_t*>(p)[at + j]) << 16);
+  return v;
+}
+
+// X_0 of a tile of 64 x 64 elements; zeros behind the matrix's sides.  The
+// matrix is read along its own rows; if those are X's columns, by way of LDS.
+constexpr uint32_t kSpread = 64;
+
+template <bool kGrad32>
+__device__ __forceinline__ f32x4 spread_four(const MuonArgs& a, const MuonRec& r, const fr_muon_hyper& h, float scale,
+                                             double f, uint32_t row, uint32_t col, uint32_t rows) {
+  if (row >= rows || col >= r.cols) return f32x4{0, 0, 0, 0};
+  const uint64_t at = uint64_t(row) * r.cols + col;
+  const uint32_t left = r.cols - col;
+  f32x4 d = load_four<kGrad32>(static_cast<const uint8_t*>(a.grads) + r.grad, at, left);
+  if (a.momentum) {
+    const f32x4 m = load_four<true>(static_cast<const uint8_t*>(a.state) + r.mom, at, left);
+#pragma unroll
+    for (uint32_t j = 0; j < 4; j++)  // (a scale may be NaN)
+      d[j] = j < left ? direction(d[j] * scale, m[j], h.momentum, h.nesterov != 0) : 0.0f;
+  }
+#pragma unroll
+  for (uint32_t j = 0; j < 4; j++) d[j] = j < left ? float(double(d[j]) * f) : 0.0f;
+  return d;
+}
+
 __global__ __launch_bounds__(256) void k_muon_spread(MuonArgs a) {
   if (a.stats->nonfinite) return;
   const uint64_t tile = a.spread.d[blockIdx.x];
-  const uint32_t id = uint32_t(tile >> 32), i0 = uint32_t(tile >> 16 & 0xFFFF) * kMuonSide,
-                 j0 = uint32_t(tile & 0xFFFF) * kMuonSide;
+  const uint32_t id = uint32_t(tile >> 32), i0 = uint32_t(tile >> 16 & 0xFFFF) * kSpread,
+                 j0 = uint32_t(tile & 0xFFFF) * kSpread;
   const MuonRec r = a.recs[id];
   const double f = a.factors[id];
   const fr_muon_hyper h = a.hyper[r.group];
   const float scale = a.stats->scale;
-  const uint8_t* const pg = static_cast<const uint8_t*>(a.grads) + r.grad;
-  const float* const pm =
-      a.momentum ? reinterpret_cast<const float*>(static_cast<const uint8_t*>(a.state) + r.mom) : nullptr;
-  float* const xc = reinterpret_cast<float*>(a.scratch + r.xc);
-  f16* const x = reinterpret_cast<f16*>(a.scratch + r.x);
-  f16* const xt = reinterpret_cast<f16*>(a.scratch + r.xt[0]);
-  __shared__ float t[32][33];
-  for (uint32_t q = 0; q < (kMuonSide / 32) * (kMuonSide / 32); q++) {
-    const uint32_t bi = i0 + q / (kMuonSide / 32) * 32, bj = j0 + q % (kMuonSide / 32) * 32;
-    const uint32_t lo = threadIdx.x % 32, hi = threadIdx.x / 32;
-    // read along the matrix's own rows, which are X's or its columns
-    for (uint32_t k = hi; k < 32; k += 8) {
-      const uint32_t i = r.wide ? bi + k : bi + lo, j = r.wide ? bj + lo : bj + k;
-      float d = 0.0f;
-      if (i < r.m && j < r.n) {
-        const uint64_t e = r.wide ? uint64_t(i) * r.cols + j : uint64_t(j) * r.cols + i;
-        d = r.grad_f32 ? reinterpret_cast<const float*>(pg)[e]
-                       : as_f(uint32_t(reinterpret_cast<const uint16_t*>(pg)[e]) << 16);
-        if (pm) d = direction(d * scale, pm[e], h.momentum, h.nesterov != 0);
-        d = float(double(d) * f);
-      }
-      if (r.wide) t[k][lo] = d;
-      else t[lo][k] = d;
-    }
+  f16* const x = reinterpret_cast<f16*>(a.scratch + r.x[0]);
+  int8_t* const rest = reinterpret_cast<int8_t*>(a.scratch + r.rest);
+  const uint32_t lo = threadIdx.x % 16 * 4, hi = threadIdx.x / 16;
+  f32x4 v[4];
+#pragma unroll
+  for (uint32_t k = 0; k < 4; k++) {
+    const uint32_t row = (r.wide ? i0 : j0) + hi + 16 * k, col = (r.wide ? j0 : i0) + lo;
+    v[k] = r.grad_f32 ? spread_four<true>(a, r, h, scale, f, row, col, r.wide ? r.m : r.n)
+                      : spread_four<false>(a, r, h, scale, f, row, col, r.wide ? r.m : r.n);
+  }
+  if (!r.wide) {
+    __shared__ float t[kSpread][kSpread + 1];
+#pragma unroll
+    for (uint32_t k = 0; k < 4; k++)
+#pragma unroll
+      for (uint32_t j = 0; j < 4; j++) t[lo + j][hi + 16 * k] = v[k][j];
     __syncthreads();
-    for (uint32_t k = hi; k < 32; k += 8) {
-      const uint64_t e = uint64_t(bi + k) * r.np + bj + lo;
-      xc[e] = t[k][lo];
-      x[e] = f16(t[k][lo]);
-      xt[uint64_t(bj + k) * r.mp + bi + lo] = f16(t[lo][k]);
+#pragma unroll
+    for (uint32_t k = 0; k < 4; k++)
+#pragma unroll
+      for (uint32_t j = 0; j < 4; j++) v[k][j] = t[hi + 16 * k][lo + j];
+  }
+#pragma unroll
+  for (uint32_t k = 0; k < 4; k++) {
+    const uint64_t at = uint64_t(i0 + hi + 16 * k) * r.np + j0 + lo;
+    f16x4 y;
+    i8x4 z;
+#pragma unroll
+    for (uint32_t j = 0; j < 4; j++) {
+      y[j] = f16(v[k][j]);
+      z[j] = rest_of(v[k][j], y[j]);
     }
-    __syncthreads();
+    *reinterpret_cast<f16x4*>(x + at) = y;
+    *reinterpret_cast<i8x4*>(rest + at) = z;
   }
 }
 
@@ -225,115 +296,226 @@ struct ProductArgs {
   uint8_t* updates;
   const fr_grad_stats* stats;
   float a, b, c;
-  uint32_t flip;      // which transpose is read; the other is written
-  uint32_t carried;   // X is read as carried, else in fp16
-  uint32_t carry;     // and is carried on
+  uint32_t flip;     // which X is read; the other is written
+  uint32_t carried;  // X has a rest
+  uint32_t carry;    // and gets one
   uint32_t last;
 };
 
-// One 128 x 128 tile of L R^T, both with their sums' index contiguous: 4 waves of
-// 64 x 64, 64 of the sum at a time in LDS, where chunks of 16 bytes are permuted by
-// their row so that 16 rows of a column of chunks lie in different banks.
-constexpr uint32_t kSide = kMuonSide, kDeep = 64;
+// How a workgroup makes a tile of B x B elements: waves of WM x WN, kStages slices
+// of the sum, kDeep deep, in LDS.
+template <uint32_t B_, uint32_t WM_, uint32_t WN_, uint32_t S_>
+struct Shape {
+  static constexpr uint32_t B = B_, WM = WM_, WN = WN_, S = S_;
+  static constexpr uint32_t waves = B / WM * (B / WN), threads = 64 * waves;
+};
+typedef Shape<256, 128, 64, 2> Large;
+typedef Shape<64, 32, 32, 4> Small;
+constexpr uint32_t kDeep = 64;
 
 typedef __attribute__((address_space(3))) void lds_void;
 typedef const __attribute__((address_space(1))) void global_void;
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
 
-__device__ __forceinline__ void fetch(const f16* src, uint64_t ld, uint32_t k0, f16* lds) {
+// A slice of an operand whose rows run along the sum: B rows of kDeep.  Chunks of
+// 16 bytes are permuted by their row, so that 16 rows of a column of chunks lie
+// in different banks.
+template <class T>
+__device__ __forceinline__ void fetch_rows(const f16* src, uint64_t ld, f16* lds) {
   const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64;
 #pragma unroll
-  for (uint32_t p = 0; p < kSide / 32; p++) {
-    const uint32_t row0 = (p * 4 + wave) * 8, row = row0 + lane / 8, chunk = (lane % 8) ^ (row / 2 % 8);
-    __builtin_amdgcn_global_load_lds((global_void*)(src + row * ld + k0 + chunk * 8), (lds_void*)(lds + row0 * kDeep),
-                                     16, 0, 0);
+  for (uint32_t p = 0; p < T::B / 8 / T::waves; p++) {
+    const uint32_t row0 = (p * T::waves + wave) * 8, row = row0 + lane / 8, chunk = (lane % 8) ^ (row / 2 % 8);
+    __builtin_amdgcn_global_load_lds((global_void*)(src + row * ld + chunk * 8), (lds_void*)(lds + row0 * kDeep), 16, 0,
+                                     0);
   }
 }
+__device__ __forceinline__ f16x8 operand_of_row(const f16* lds, uint32_t row, uint32_t chunk) {
+  return *reinterpret_cast<const f16x8*>(lds + row * kDeep + (chunk ^ (row / 2 % 8)) * 8);
+}
 
-template <Product kWhat>
-__global__ __launch_bounds__(256) void k_muon_product(ProductArgs p) {
+// A slice of one whose columns run along the sum: kDeep rows of B, pairs of
+// chunks (16 columns) permuted so that four rows of them lie in different banks.
+template <class T>
+__device__ __forceinline__ uint32_t pair_of(uint32_t row) {
+  return T::B == 64 ? row / 2 % 4 : row % 8;
+}
+template <class T>
+__device__ __forceinline__ void fetch_columns(const f16* src, uint64_t ld, f16* lds) {
+  constexpr uint32_t chunks = T::B / 8, rows = 64 / chunks;  // of a row, of a wave's load
+  const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+#pragma unroll
+  for (uint32_t p = 0; p < kDeep / rows / T::waves; p++) {
+    const uint32_t row0 = (p * T::waves + wave) * rows, row = row0 + lane / chunks;
+    const uint32_t chunk = (lane % chunks) ^ (pair_of<T>(row) * 2);
+    __builtin_amdgcn_global_load_lds((global_void*)(src + row * ld + chunk * 8), (lds_void*)(lds + row0 * T::B), 16, 0,
+                                     0);
+  }
+}
+// Rows 32 kk + 8 quad ... + 7 of the lane's column of 16 from `col` on: a
+// transposing read gives a lane four rows of its column for which the 16 lanes
+// name four rows of 16 columns.
+template <class T>
+__device__ __forceinline__ f16x8 operand_of_columns(const f16* lds, uint32_t col, uint32_t kk) {
+  const uint32_t lane = threadIdx.x % 64, quad = lane / 16, i = lane % 16;
+  const uint32_t row = kk * 32 + quad * 8 + i / 4;
+  union {
+    f16x8 v;
+    i16x4 half[2];
+  } u;
+#pragma unroll
+  for (uint32_t h = 0; h < 2; h++) {
+    const uint32_t k = row + 4 * h;
+    u.half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (lds_i16x4*)(lds + k * T::B + ((col / 16) ^ pair_of<T>(k)) * 16 + i % 4 * 4));
+  }
+  return u.v;
+}
+
+// All of a wave's reads of LDS are done, and all but its last `left` loads into it.
+template <uint32_t kLeft>
+__device__ __forceinline__ void arrive() {
+  static_assert(kLeft < 64, "six bits");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLeft) : "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// One tile of L R (kWhole, with R's columns along the sum) or L R^T.
+template <Product kWhat, class T>
+__global__ __launch_bounds__(T::threads) void k_muon_product(ProductArgs p) {
   if (p.stats->nonfinite) return;
-  __shared__ __attribute__((aligned(16))) f16 lds[2][2][kSide * kDeep];
+  extern __shared__ __attribute__((aligned(16))) f16 lds[];
+  constexpr uint32_t kSlice = T::B * kDeep, M = T::WM / 16, N = T::WN / 16;
+  constexpr uint32_t kLoads = 2 * kSlice / (8 * T::threads);  // of a wave, a slice of both operands
   const uint64_t tile = p.tiles[blockIdx.x];
   const MuonRec r = p.recs[tile >> 32];
-  const uint32_t i0 = uint32_t(tile >> 16 & 0xFFFF) * kSide, j0 = uint32_t(tile & 0xFFFF) * kSide;
-  f16* const X = reinterpret_cast<f16*>(p.scratch + r.x);
+  const uint32_t i0 = uint32_t(tile >> 16 & 0xFFFF) * T::B, j0 = uint32_t(tile & 0xFFFF) * T::B;
+  f16* const X = reinterpret_cast<f16*>(p.scratch + (p.flip ? r.x[1] : r.x[0]));
   f16* const A = reinterpret_cast<f16*>(p.scratch + r.a);
   f16* const Q = reinterpret_cast<f16*>(p.scratch + r.q);
-  f16* const from = reinterpret_cast<f16*>(p.scratch + (p.flip ? r.xt[1] : r.xt[0]));
-  f16* const to = reinterpret_cast<f16*>(p.scratch + (p.flip ? r.xt[0] : r.xt[1]));
-  const f16* const L = kWhat == kGram ? X : kWhat == kPoly ? A : Q;
-  const f16* const R = kWhat == kGram ? X : kWhat == kPoly ? A : from;
   const uint32_t K = kWhat == kGram ? r.np : r.mp;
-  const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64, wi = wave / 2 * 64, wj = wave % 2 * 64;
+  const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+  const uint32_t wi = wave / (T::B / T::WN) * T::WM, wj = wave % (T::B / T::WN) * T::WN;
   const uint32_t row = lane % 16, quad = lane / 16;
-  const f16* const pl = L + uint64_t(i0) * K;
-  const f16* const pr = R + uint64_t(j0) * K;
-  f32x4 acc[4][4] = {};
-  fetch(pl, K, 0, lds[0][0]);
-  fetch(pr, K, 0, lds[0][1]);
-  for (uint32_t k = 0, b = 0; k < K; k += kDeep, b ^= 1) {
-    __syncthreads();  // (waits for this wave's loads into LDS as well)
-    if (k + kDeep < K) {
-      fetch(pl, K, k + kDeep, lds[b ^ 1][0]);
-      fetch(pr, K, k + kDeep, lds[b ^ 1][1]);
-    }
+  const f16* const pl = (kWhat == kGram ? X : kWhat == kPoly ? A : Q) + uint64_t(i0) * K;
+  const f16* const pr = kWhat == kWhole ? X + j0 : (kWhat == kGram ? X : A) + uint64_t(j0) * K;
+  const auto fetch = [&](uint32_t k) {
+    f16* const to = lds + k / kDeep % T::S * 2 * kSlice;
+    fetch_rows<T>(pl + k, K, to);
+    if constexpr (kWhat == kWhole) fetch_columns<T>(pr + uint64_t(k) * r.np, r.np, to + kSlice);
+    else fetch_rows<T>(pr + k, K, to + kSlice);
+  };
+  f32x4 acc[M][N] = {};
+  // (the slices past the end are not loaded: then fewer are in flight than waited
+  // for, so that the last ones wait for all)
 #pragma unroll
-    for (uint32_t kk = 0; kk < 2; kk++) {
-      f16x8 x[4], y[4];
+  for (uint32_t s = 0; s + 1 < T::S; s++)
+    if (s * kDeep < K) fetch(s * kDeep);
+  for (uint32_t k = 0; k < K; k += kDeep) {
+    if (k + (T::S - 1) * kDeep <= K) arrive<(T::S - 2) * kLoads>();
+    else arrive<0>();
+    if (k + (T::S - 1) * kDeep < K) fetch(k + (T::S - 1) * kDeep);
+    const f16* const from = lds + k / kDeep % T::S * 2 * kSlice;
 #pragma unroll
-      for (uint32_t q = 0; q < 4; q++) {
-        const uint32_t ri = wi + q * 16 + row, rj = wj + q * 16 + row, ch = kk * 4 + quad;
-        x[q] = *reinterpret_cast<const f16x8*>(&lds[b][0][ri * kDeep + (ch ^ (ri / 2 % 8)) * 8]);
-        y[q] = *reinterpret_cast<const f16x8*>(&lds[b][1][rj * kDeep + (ch ^ (rj / 2 % 8)) * 8]);
-      }
+    for (uint32_t kk = 0; kk < kDeep / 32; kk++) {
+      f16x8 x[M], y[N];
 #pragma unroll
-      for (uint32_t s = 0; s < 4; s++)
+      for (uint32_t q = 0; q < N; q++)
+        y[q] = kWhat == kWhole ? operand_of_columns<T>(from + kSlice, wj + q * 16, kk)
+                               : operand_of_row(from + kSlice, wj + q * 16 + row, kk * 4 + quad);
 #pragma unroll
-        for (uint32_t q = 0; q < 4; q++)
-          acc[s][q] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[s], y[q], acc[s][q], 0, 0, 0);
+      for (uint32_t s = 0; s < M; s++) x[s] = operand_of_row(from, wi + s * 16 + row, kk * 4 + quad);
+#pragma unroll
+      for (uint32_t s = 0; s < M; s++)
+#pragma unroll
+        for (uint32_t q = 0; q < N; q++)
+          acc[s][q] = __builtin_amdgcn_mfma_f32_16x16x32_f16(y[q], x[s], acc[s][q], 0, 0, 0);
     }
   }
-  // a lane holds rows 4 quad ... 4 quad + 3 of column `row` of each 16 x 16
-  float* const xc = reinterpret_cast<float*>(p.scratch + r.xc);
+  // a lane holds columns 4 quad ... 4 quad + 3 of row `row` of each 16 x 16
+  f16* const to = reinterpret_cast<f16*>(p.scratch + (p.flip ? r.x[0] : r.x[1]));
+  int8_t* const rest = reinterpret_cast<int8_t*>(p.scratch + r.rest);
 #pragma unroll
-  for (uint32_t s = 0; s < 4; s++)
+  for (uint32_t s = 0; s < M; s++)
 #pragma unroll
-    for (uint32_t q = 0; q < 4; q++) {
-      const uint32_t i = i0 + wi + s * 16 + quad * 4, j = j0 + wj + q * 16 + row;
+    for (uint32_t q = 0; q < N; q++) {
+      const uint32_t i = i0 + wi + s * 16 + row, j = j0 + wj + q * 16 + quad * 4;
       f32x4 v = acc[s][q];
       f16x4 h;
       if constexpr (kWhat == kWhole) {
+        const uint64_t at = uint64_t(i) * r.np + j;
+        const f16x4 x = *reinterpret_cast<const f16x4*>(X + at);
+        i8x4 z = {};
+        if (p.carried) z = *reinterpret_cast<const i8x4*>(rest + at);
 #pragma unroll
         for (uint32_t e = 0; e < 4; e++) {
-          const uint64_t at = uint64_t(i + e) * r.np + j;
-          const float x = p.carried ? xc[at] : float(X[at]);
-          v[e] = __builtin_fmaf(p.a, x, v[e] * (1.0f / kMuonLiftA));
-          if (p.carry) xc[at] = v[e];
+          v[e] = __builtin_fmaf(p.a, p.carried ? with_rest(x[e], z[e]) : float(x[e]), v[e] * (1.0f / kMuonLiftA));
           h[e] = f16(v[e]);
-          if (!p.last) X[at] = h[e];
+          if (p.carry) z[e] = rest_of(v[e], h[e]);
         }
         if (!p.last) {
-          *reinterpret_cast<f16x4*>(to + uint64_t(j) * r.mp + i) = h;
-        } else if (j < r.n) {
+          *reinterpret_cast<f16x4*>(to + at) = h;
+          if (p.carry) *reinterpret_cast<i8x4*>(rest + at) = z;
+        } else if (i < r.m && j < r.n) {
           uint16_t* const out = reinterpret_cast<uint16_t*>(p.updates + r.update);
-          for (uint32_t e = 0; e < 4; e++)
-            if (i + e < r.m)
-              out[r.wide ? uint64_t(i + e) * r.cols + j : uint64_t(j) * r.cols + i + e] =
-                  uint16_t(rne_bf16(as_u(v[e] * (1.0f / r.lift))));
+          v *= 1.0f / r.lift;
+          if (r.wide && r.cols % 4 == 0) {
+            *reinterpret_cast<u32x2*>(out + uint64_t(i) * r.cols + j) = to_bf16(v);
+          } else {
+#pragma unroll
+            for (uint32_t e = 0; e < 4; e++)
+              if (j + e < r.n)
+                out[r.wide ? uint64_t(i) * r.cols + j + e : uint64_t(j + e) * r.cols + i] = uint16_t(rne_bf16(as_u(v[e])));
+          }
         }
       } else {
         f16* const out = kWhat == kGram ? A : Q;
+        const uint64_t at = uint64_t(i) * r.mp + j;
+        if constexpr (kWhat == kGram) {
+          v *= kMuonLiftA / (r.lift * r.lift);
+        } else {
+          const f16x4 x = *reinterpret_cast<const f16x4*>(A + at);
 #pragma unroll
-        for (uint32_t e = 0; e < 4; e++) {
-          const uint64_t at = uint64_t(i + e) * r.mp + j;
-          if constexpr (kWhat == kGram) v[e] *= kMuonLiftA / (r.lift * r.lift);
-          else v[e] = __builtin_fmaf(p.b, float(A[at]), p.c * (1.0f / kMuonLiftA) * v[e]);
-          h[e] = f16(v[e]);
-          out[at] = h[e];
+          for (uint32_t e = 0; e < 4; e++) v[e] = __builtin_fmaf(p.b, float(x[e]), p.c * (1.0f / kMuonLiftA) * v[e]);
         }
-        if (i0 != j0) *reinterpret_cast<f16x4*>(out + uint64_t(j) * r.mp + i) = h;
+#pragma unroll
+        for (uint32_t e = 0; e < 4; e++) h[e] = f16(v[e]);
+        *reinterpret_cast<f16x4*>(out + at) = h;
+        if (i0 != j0)
+#pragma unroll
+          for (uint32_t e = 0; e < 4; e++) out[uint64_t(j + e) * r.mp + i] = h[e];
       }
     }
+}
+
+template <class T>
+int products(const MuonArgs& a, hipStream_t st) {
+  constexpr uint32_t lds = T::S * 2 * T::B * kDeep * sizeof(f16);
+  for (uint32_t s = 0; s < a.n_steps; s++) {
+    ProductArgs p;
+    p.recs = a.recs;
+    p.scratch = a.scratch;
+    p.updates = static_cast<uint8_t*>(a.updates);
+    p.stats = a.stats;
+    p.a = a.coeffs[s].a;
+    p.b = a.coeffs[s].b;
+    p.c = a.coeffs[s].c;
+    p.flip = s & 1;
+    p.last = s + 1 == a.n_steps;
+    p.carried = s == 0 || s + 2 < a.n_steps;
+    p.carry = s + 3 < a.n_steps;
+    p.tiles = a.gram.d;
+    hipLaunchKernelGGL((k_muon_product<kGram, T>), dim3(uint32_t(a.gram.n)), dim3(T::threads), lds, st, p);
+    if (const int e = int(hipGetLastError())) return e;
+    hipLaunchKernelGGL((k_muon_product<kPoly, T>), dim3(uint32_t(a.gram.n)), dim3(T::threads), lds, st, p);
+    if (const int e = int(hipGetLastError())) return e;
+    p.tiles = a.whole.d;
+    hipLaunchKernelGGL((k_muon_product<kWhole, T>), dim3(uint32_t(a.whole.n)), dim3(T::threads), lds, st, p);
+    if (const int e = int(hipGetLastError())) return e;
+  }
+  return 0;
 }
 
 int fold(const MuonArgs& a, hipStream_t st) {
@@ -363,29 +545,7 @@ int launch_muon_direction(const MuonArgs& a, void* stream) {
   if (const int e = int(hipGetLastError())) return e;
   hipLaunchKernelGGL(k_muon_spread, dim3(uint32_t(a.spread.n)), dim3(256), 0, st, a);
   if (const int e = int(hipGetLastError())) return e;
-  for (uint32_t s = 0; s < a.n_steps; s++) {
-    ProductArgs p;
-    p.recs = a.recs;
-    p.scratch = a.scratch;
-    p.updates = static_cast<uint8_t*>(a.updates);
-    p.stats = a.stats;
-    p.a = a.coeffs[s].a;
-    p.b = a.coeffs[s].b;
-    p.c = a.coeffs[s].c;
-    p.flip = s & 1;
-    p.last = s + 1 == a.n_steps;
-    p.carried = s == 0 || s + 2 < a.n_steps;
-    p.carry = s + 3 < a.n_steps;
-    p.tiles = a.gram.d;
-    hipLaunchKernelGGL(k_muon_product<kGram>, dim3(uint32_t(a.gram.n)), dim3(256), 0, st, p);
-    if (const int e = int(hipGetLastError())) return e;
-    hipLaunchKernelGGL(k_muon_product<kPoly>, dim3(uint32_t(a.gram.n)), dim3(256), 0, st, p);
-    if (const int e = int(hipGetLastError())) return e;
-    p.tiles = a.whole.d;
-    hipLaunchKernelGGL(k_muon_product<kWhole>, dim3(uint32_t(a.whole.n)), dim3(256), 0, st, p);
-    if (const int e = int(hipGetLastError())) return e;
-  }
-  return 0;
+  return a.side == kMuonLarge ? products<Large>(a, st) : products<Small>(a, st);
 }
 
 int launch_muon_apply(const MuonArgs& a, void* stream) {
