@@ -3,6 +3,8 @@
 // step along the updates.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "device.h"
 #include "elements.h"
 #include "muon.h"
@@ -313,62 +315,100 @@ typedef Shape<256, 128, 64, 2> Large;
 typedef Shape<64, 32, 32, 4> Small;
 constexpr uint32_t kDeep = 64;
 
-typedef __attribute__((address_space(3))) void lds_void;
-typedef const __attribute__((address_space(1))) void global_void;
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
 
-// A slice of an operand whose rows run along the sum: B rows of kDeep.  Chunks of
-// 16 bytes are permuted by their row, so that 16 rows of a column of chunks lie
-// in different banks.
-template <class T>
-__device__ __forceinline__ void fetch_rows(const f16* src, uint64_t ld, f16* lds) {
-  const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64;
-#pragma unroll
-  for (uint32_t p = 0; p < T::B / 8 / T::waves; p++) {
-    const uint32_t row0 = (p * T::waves + wave) * 8, row = row0 + lane / 8, chunk = (lane % 8) ^ (row / 2 % 8);
-    __builtin_amdgcn_global_load_lds((global_void*)(src + row * ld + chunk * 8), (lds_void*)(lds + row0 * kDeep), 16, 0,
-                                     0);
-  }
-}
-__device__ __forceinline__ f16x8 operand_of_row(const f16* lds, uint32_t row, uint32_t chunk) {
-  return *reinterpret_cast<const f16x8*>(lds + row * kDeep + (chunk ^ (row / 2 % 8)) * 8);
+__device__ __forceinline__ uint32_t lds_address(const f16* p) {
+  return uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const f16*)p));
 }
 
-// A slice of one whose columns run along the sum: kDeep rows of B, pairs of
-// chunks (16 columns) permuted so that four rows of them lie in different banks.
-template <class T>
-__device__ __forceinline__ uint32_t pair_of(uint32_t row) {
-  return T::B == 64 ? row / 2 % 4 : row % 8;
+// A wave's load into LDS: lane l's 16 bytes from base + offset to `to` + 16 l.  (As
+// a builtin it makes the compiler wait for all such loads before each transposing
+// read, which it takes to read what they write; arrive() waits for them.  The
+// compiler itself has no use for m0 in these kernels, which the tests make sure
+// of.)
+__device__ __forceinline__ void load_to_lds(const f16* base, uint32_t offset, const f16* to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_address(to)), "v"(offset),
+               "s"(base)
+               : "memory");
 }
+
+// Which column of L R^T a lane of operand R stands for.  Of the 16 columns of a
+// matrix instruction's result a lane holds four in turn; the N of them that a
+// wave has side by side are interleaved, so that it holds 4 N in turn of a row.
 template <class T>
-__device__ __forceinline__ void fetch_columns(const f16* src, uint64_t ld, f16* lds) {
-  constexpr uint32_t chunks = T::B / 8, rows = 64 / chunks;  // of a row, of a wave's load
-  const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64;
-#pragma unroll
-  for (uint32_t p = 0; p < kDeep / rows / T::waves; p++) {
-    const uint32_t row0 = (p * T::waves + wave) * rows, row = row0 + lane / chunks;
-    const uint32_t chunk = (lane % chunks) ^ (pair_of<T>(row) * 2);
-    __builtin_amdgcn_global_load_lds((global_void*)(src + row * ld + chunk * 8), (lds_void*)(lds + row0 * T::B), 16, 0,
-                                     0);
+__device__ __forceinline__ uint32_t column_of(uint32_t q, uint32_t lane) {
+  return lane / 4 * (T::WN / 4) + q * 4 + lane % 4;
+}
+
+// A slice of an operand whose rows run along the sum: B rows of kDeep.  Chunks of
+// 16 bytes are permuted by their row, so that the 16 rows whose chunk is read at
+// one time lie in different banks: rows in turn of L, column_of's of R.
+template <class T, bool kR>
+__device__ __forceinline__ uint32_t row_key(uint32_t row) {
+  return kR ? (row / 2 % 2) | row / (T::WN / 4) % 4 * 2 : row / 2 % 8;
+}
+// (One offset a lane, of the first of a wave's loads: the others' rows have the
+// same keys, and the rest of their addresses is a scalar.)
+template <class T, bool kR>
+struct Rows {
+  uint32_t offset;  // bytes
+  __device__ __forceinline__ Rows(uint32_t wave, uint32_t ld) {
+    const uint32_t lane = threadIdx.x % 64, row = wave * 8 + lane / 8;
+    static_assert(T::waves * 8 % T::WN == 0, "keys of R go by rows mod WN");
+    offset = (row * ld + ((lane % 8) ^ row_key<T, kR>(row)) * 8) * 2;
   }
+  __device__ __forceinline__ void fetch(const f16* src, uint32_t ld, f16* lds, uint32_t wave) const {
+#pragma unroll
+    for (uint32_t p = 0; p < T::B / 8 / T::waves; p++)
+      load_to_lds(src + uint64_t(p * T::waves * 8) * ld, offset, lds + (p * T::waves + wave) * 8 * kDeep);
+  }
+};
+template <class T, bool kR>
+__device__ __forceinline__ f16x8 operand_of_row(const f16* lds, uint32_t row, uint32_t chunk) {
+  return *reinterpret_cast<const f16x8*>(lds + row * kDeep + (chunk ^ row_key<T, kR>(row)) * 8);
 }
-// Rows 32 kk + 8 quad ... + 7 of the lane's column of 16 from `col` on: a
-// transposing read gives a lane four rows of its column for which the 16 lanes
-// name four rows of 16 columns.
+
+// A slice of R where its columns run along the sum: kDeep rows of B.  Chunks are
+// permuted so that four columns of four rows each, as read at one time, lie in
+// different banks.
 template <class T>
-__device__ __forceinline__ f16x8 operand_of_columns(const f16* lds, uint32_t col, uint32_t kk) {
+__device__ __forceinline__ uint32_t column_key(uint32_t row) {
+  constexpr uint32_t N = T::WN / 16;
+  static_assert((N == 4 && T::B == 256) || (N == 2 && T::B == 64), "the shapes there are");
+  return N == 4 ? (row & 1) | (row & 2) << 2 : (row & 2) << 1;
+}
+template <class T>
+struct Columns {
+  static constexpr uint32_t kChunks = T::B / 8, kRows = 64 / kChunks;  // of a row, of a wave's load
+  uint32_t offset;
+  __device__ __forceinline__ Columns(uint32_t wave, uint32_t ld) {
+    const uint32_t lane = threadIdx.x % 64, row = wave * kRows + lane / kChunks;
+    static_assert(T::waves * kRows % 4 == 0, "keys go by rows mod 4");
+    offset = (row * ld + ((lane % kChunks) ^ column_key<T>(row)) * 8) * 2;
+  }
+  __device__ __forceinline__ void fetch(const f16* src, uint32_t ld, f16* lds, uint32_t wave) const {
+#pragma unroll
+    for (uint32_t p = 0; p < kDeep / kRows / T::waves; p++)
+      load_to_lds(src + uint64_t(p * T::waves * kRows) * ld, offset, lds + (p * T::waves + wave) * kRows * T::B);
+  }
+};
+// Rows 32 kk + 8 quad ... + 7 of the lane's column of those from `col` on: a
+// transposing read gives a lane four rows of its column for which the 16 lanes
+// name four rows of four columns each.
+template <class T>
+__device__ __forceinline__ f16x8 operand_of_columns(const f16* lds, uint32_t col, uint32_t q, uint32_t kk) {
   const uint32_t lane = threadIdx.x % 64, quad = lane / 16, i = lane % 16;
-  const uint32_t row = kk * 32 + quad * 8 + i / 4;
+  const uint32_t c = col + column_of<T>(q, i % 4 * 4);
   union {
     f16x8 v;
     i16x4 half[2];
   } u;
 #pragma unroll
   for (uint32_t h = 0; h < 2; h++) {
-    const uint32_t k = row + 4 * h;
+    const uint32_t k = kk * 32 + quad * 8 + i / 4 + 4 * h;
     u.half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        (lds_i16x4*)(lds + k * T::B + ((col / 16) ^ pair_of<T>(k)) * 16 + i % 4 * 4));
+        (lds_i16x4*)(lds + k * T::B + ((c / 8) ^ column_key<T>(k)) * 8 + c % 8));
   }
   return u.v;
 }
@@ -380,6 +420,50 @@ __device__ __forceinline__ void arrive() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLeft) : "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
+}
+
+// A wave's operands of 32 of the sum: all N of R's, or half of the M of L's.
+template <class T, bool kColumns>
+struct Operands {
+  static constexpr uint32_t M = T::WM / 16, N = T::WN / 16, H = M / 2;
+  const uint32_t wi, wj;
+  f16x8 y[2][N], x[2][H];
+  __device__ __forceinline__ void read_r(const f16* lds, uint32_t kk) {
+    const uint32_t lane = threadIdx.x % 64;
+    const f16* const r = lds + T::B * kDeep;
+#pragma unroll
+    for (uint32_t q = 0; q < N; q++)
+      y[kk][q] = kColumns ? operand_of_columns<T>(r, wj, q, kk)
+                          : operand_of_row<T, true>(r, wj + column_of<T>(q, lane % 16), kk * 4 + lane / 16);
+  }
+  __device__ __forceinline__ void read_l(const f16* lds, uint32_t kk, uint32_t half) {
+    const uint32_t lane = threadIdx.x % 64;
+#pragma unroll
+    for (uint32_t s = 0; s < H; s++)
+      x[half][s] = operand_of_row<T, false>(lds, wi + (half * H + s) * 16 + lane % 16, kk * 4 + lane / 16);
+  }
+  __device__ __forceinline__ void multiply(f32x4 (&acc)[M][N], uint32_t kk, uint32_t half) const {
+#pragma unroll
+    for (uint32_t s = 0; s < H; s++)
+#pragma unroll
+      for (uint32_t q = 0; q < N; q++)
+        acc[half * H + s][q] =
+            __builtin_amdgcn_mfma_f32_16x16x32_f16(y[kk][q], x[half][s], acc[half * H + s][q], 0, 0, 0);
+  }
+};
+
+// The order of what stands before it: one of kReads reads of LDS, then its share
+// of kProducts matrix instructions.
+template <uint32_t kReads, uint32_t kProducts>
+__device__ __forceinline__ void interleave() {
+  constexpr uint32_t each = kProducts / kReads ? kProducts / kReads : 1;
+#pragma unroll
+  for (uint32_t i = 0; i < kReads; i++) {
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x008, each, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, kProducts, 0);
+  __builtin_amdgcn_sched_barrier(0);
 }
 
 // One tile of L R (kWhole, with R's columns along the sum) or L R^T.
@@ -396,98 +480,154 @@ __global__ __launch_bounds__(T::threads) void k_muon_product(ProductArgs p) {
   f16* const A = reinterpret_cast<f16*>(p.scratch + r.a);
   f16* const Q = reinterpret_cast<f16*>(p.scratch + r.q);
   const uint32_t K = kWhat == kGram ? r.np : r.mp;
-  const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
   const uint32_t wi = wave / (T::B / T::WN) * T::WM, wj = wave % (T::B / T::WN) * T::WN;
-  const uint32_t row = lane % 16, quad = lane / 16;
   const f16* const pl = (kWhat == kGram ? X : kWhat == kPoly ? A : Q) + uint64_t(i0) * K;
   const f16* const pr = kWhat == kWhole ? X + j0 : (kWhat == kGram ? X : A) + uint64_t(j0) * K;
+  const Rows<T, false> left(wave, K);
+  const std::conditional_t<kWhat == kWhole, Columns<T>, Rows<T, true>> right(wave, kWhat == kWhole ? r.np : K);
+  const auto slice = [&](uint32_t k) { return lds + k / kDeep % T::S * 2 * kSlice; };
   const auto fetch = [&](uint32_t k) {
-    f16* const to = lds + k / kDeep % T::S * 2 * kSlice;
-    fetch_rows<T>(pl + k, K, to);
-    if constexpr (kWhat == kWhole) fetch_columns<T>(pr + uint64_t(k) * r.np, r.np, to + kSlice);
-    else fetch_rows<T>(pr + k, K, to + kSlice);
+    left.fetch(pl + k, K, slice(k), wave);
+    if constexpr (kWhat == kWhole) right.fetch(pr + uint64_t(k) * r.np, r.np, slice(k) + kSlice, wave);
+    else right.fetch(pr + k, K, slice(k) + kSlice, wave);
   };
   f32x4 acc[M][N] = {};
-  // (the slices past the end are not loaded: then fewer are in flight than waited
-  // for, so that the last ones wait for all)
+  Operands<T, kWhat == kWhole> o{wi, wj};
+  // What is multiplied next is read while something else is: halves of L's rows,
+  // and R's columns for the next 32 of the sum.
+  const auto first_three = [&](const f16* from) {
+    o.read_l(from, 0, 1);
+    o.read_r(from, 1);
+    o.multiply(acc, 0, 0);
+    interleave<M / 2 + (kWhat == kWhole ? 2 : 1) * N, M * N / 2>();
+    o.read_l(from, 1, 0);
+    o.multiply(acc, 0, 1);
+    interleave<M / 2, M * N / 2>();
+    o.read_l(from, 1, 1);
+    o.multiply(acc, 1, 0);
+    interleave<M / 2, M * N / 2>();
+  };
+  const auto last_one = [&](const f16* next) {
+    o.read_r(next, 0);
+    o.read_l(next, 0, 0);
+    o.multiply(acc, 1, 1);
+    interleave<M / 2 + (kWhat == kWhole ? 2 : 1) * N, M * N / 2>();
+  };
 #pragma unroll
-  for (uint32_t s = 0; s + 1 < T::S; s++)
+  for (uint32_t s = 0; s < T::S; s++)
     if (s * kDeep < K) fetch(s * kDeep);
-  for (uint32_t k = 0; k < K; k += kDeep) {
-    if (k + (T::S - 1) * kDeep <= K) arrive<(T::S - 2) * kLoads>();
-    else arrive<0>();
-    if (k + (T::S - 1) * kDeep < K) fetch(k + (T::S - 1) * kDeep);
-    const f16* const from = lds + k / kDeep % T::S * 2 * kSlice;
-#pragma unroll
-    for (uint32_t kk = 0; kk < kDeep / 32; kk++) {
-      f16x8 x[M], y[N];
-#pragma unroll
-      for (uint32_t q = 0; q < N; q++)
-        y[q] = kWhat == kWhole ? operand_of_columns<T>(from + kSlice, wj + q * 16, kk)
-                               : operand_of_row(from + kSlice, wj + q * 16 + row, kk * 4 + quad);
-#pragma unroll
-      for (uint32_t s = 0; s < M; s++) x[s] = operand_of_row(from, wi + s * 16 + row, kk * 4 + quad);
-#pragma unroll
-      for (uint32_t s = 0; s < M; s++)
-#pragma unroll
-        for (uint32_t q = 0; q < N; q++)
-          acc[s][q] = __builtin_amdgcn_mfma_f32_16x16x32_f16(y[q], x[s], acc[s][q], 0, 0, 0);
-    }
+  if (T::S * kDeep <= K) arrive<(T::S - 1) * kLoads>();
+  else arrive<0>();
+  o.read_r(slice(0), 0);
+  o.read_l(slice(0), 0, 0);
+  uint32_t k = 0;
+  for (; k + T::S * kDeep < K; k += kDeep) {
+    first_three(slice(k));
+    arrive<(T::S - 2) * kLoads>();  // the next slice is there, and nobody reads this one any more
+    fetch(k + T::S * kDeep);
+    last_one(slice(k + kDeep));
   }
-  // a lane holds columns 4 quad ... 4 quad + 3 of row `row` of each 16 x 16
+  for (; k + kDeep < K; k += kDeep) {  // nothing is left to load: waits for all
+    first_three(slice(k));
+    arrive<0>();
+    last_one(slice(k + kDeep));
+  }
+  first_three(slice(k));
+  o.multiply(acc, 1, 1);
+
+  // of rows wi + 16 s + lane % 16 a lane holds 4 N columns in turn
   f16* const to = reinterpret_cast<f16*>(p.scratch + (p.flip ? r.x[0] : r.x[1]));
   int8_t* const rest = reinterpret_cast<int8_t*>(p.scratch + r.rest);
+  const uint32_t i1 = i0 + wi + lane % 16, j = j0 + wj + lane / 16 * 4 * N;
+  typedef f16 f16xN __attribute__((ext_vector_type(4 * N)));
+  typedef int8_t i8xN __attribute__((ext_vector_type(4 * N)));
+  if constexpr (kWhat == kWhole) {
+    const auto finish = [&](auto carried, auto carry, auto last) {
+      constexpr uint32_t G = M < 4 ? M : 4;  // rows' loads in flight together
+      f16xN x[G];
+      i8xN z[G];
 #pragma unroll
-  for (uint32_t s = 0; s < M; s++)
-#pragma unroll
-    for (uint32_t q = 0; q < N; q++) {
-      const uint32_t i = i0 + wi + s * 16 + row, j = j0 + wj + q * 16 + quad * 4;
-      f32x4 v = acc[s][q];
-      f16x4 h;
-      if constexpr (kWhat == kWhole) {
+      for (uint32_t s = 0; s < M; s++) {
+        const uint32_t i = i1 + 16 * s, g = s % G;
         const uint64_t at = uint64_t(i) * r.np + j;
-        const f16x4 x = *reinterpret_cast<const f16x4*>(X + at);
-        i8x4 z = {};
-        if (p.carried) z = *reinterpret_cast<const i8x4*>(rest + at);
+        if (g == 0) {
+          __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (uint32_t e = 0; e < 4; e++) {
-          v[e] = __builtin_fmaf(p.a, p.carried ? with_rest(x[e], z[e]) : float(x[e]), v[e] * (1.0f / kMuonLiftA));
-          h[e] = f16(v[e]);
-          if (p.carry) z[e] = rest_of(v[e], h[e]);
-        }
-        if (!p.last) {
-          *reinterpret_cast<f16x4*>(to + at) = h;
-          if (p.carry) *reinterpret_cast<i8x4*>(rest + at) = z;
-        } else if (i < r.m && j < r.n) {
-          uint16_t* const out = reinterpret_cast<uint16_t*>(p.updates + r.update);
-          v *= 1.0f / r.lift;
-          if (r.wide && r.cols % 4 == 0) {
-            *reinterpret_cast<u32x2*>(out + uint64_t(i) * r.cols + j) = to_bf16(v);
-          } else {
-#pragma unroll
-            for (uint32_t e = 0; e < 4; e++)
-              if (j + e < r.n)
-                out[r.wide ? uint64_t(i) * r.cols + j + e : uint64_t(j + e) * r.cols + i] = uint16_t(rne_bf16(as_u(v[e])));
+          for (uint32_t n = 0; n < G; n++) {
+            x[n] = *reinterpret_cast<const f16xN*>(X + at + uint64_t(16 * n) * r.np);
+            if constexpr (carried) z[n] = *reinterpret_cast<const i8xN*>(rest + at + uint64_t(16 * n) * r.np);
           }
         }
-      } else {
-        f16* const out = kWhat == kGram ? A : Q;
-        const uint64_t at = uint64_t(i) * r.mp + j;
-        if constexpr (kWhat == kGram) {
-          v *= kMuonLiftA / (r.lift * r.lift);
-        } else {
-          const f16x4 x = *reinterpret_cast<const f16x4*>(A + at);
+        float v[4 * N];
+        f16xN h;
 #pragma unroll
-          for (uint32_t e = 0; e < 4; e++) v[e] = __builtin_fmaf(p.b, float(x[e]), p.c * (1.0f / kMuonLiftA) * v[e]);
+        for (uint32_t e = 0; e < 4 * N; e++) {
+          float was;
+          if constexpr (carried) was = with_rest(x[g][e], z[g][e]);
+          else was = float(x[g][e]);
+          v[e] = __builtin_fmaf(p.a, was, acc[s][e / 4][e % 4] * (1.0f / kMuonLiftA));
+          h[e] = f16(v[e]);
+          if constexpr (carry) z[g][e] = rest_of(v[e], h[e]);
         }
+        if constexpr (!last) {
+          *reinterpret_cast<f16xN*>(to + at) = h;
+          if constexpr (carry) *reinterpret_cast<i8xN*>(rest + at) = z[g];
+        } else if (i < r.m && j < r.n) {
+          uint16_t* const out = reinterpret_cast<uint16_t*>(p.updates + r.update);
+          const float down = 1.0f / r.lift;
+          if (r.wide && r.cols % 8 == 0) {
 #pragma unroll
-        for (uint32_t e = 0; e < 4; e++) h[e] = f16(v[e]);
-        *reinterpret_cast<f16x4*>(out + at) = h;
-        if (i0 != j0)
+            for (uint32_t e = 0; e < 4 * N; e += 8)
+              if (j + e < r.n) {
+                const u32x2 lo = to_bf16(f32x4{v[e] * down, v[e + 1] * down, v[e + 2] * down, v[e + 3] * down});
+                const u32x2 hi = to_bf16(f32x4{v[e + 4] * down, v[e + 5] * down, v[e + 6] * down, v[e + 7] * down});
+                *reinterpret_cast<u32x4*>(out + uint64_t(i) * r.cols + j + e) = u32x4{lo.x, lo.y, hi.x, hi.y};
+              }
+          } else {
 #pragma unroll
-          for (uint32_t e = 0; e < 4; e++) out[uint64_t(j + e) * r.mp + i] = h[e];
+            for (uint32_t e = 0; e < 4 * N; e++)
+              if (j + e < r.n)
+                out[r.wide ? uint64_t(i) * r.cols + j + e : uint64_t(j + e) * r.cols + i] =
+                    uint16_t(rne_bf16(as_u(v[e] * down)));
+          }
+        }
       }
+    };
+    constexpr std::true_type yes;
+    constexpr std::false_type no;
+    if (p.last) {
+      if (p.carried) finish(yes, no, yes);
+      else finish(no, no, yes);
+    } else if (p.carry) {
+      finish(yes, yes, no);
+    } else if (p.carried) {
+      finish(yes, no, no);
+    } else {
+      finish(no, no, no);
     }
+  } else {
+    f16* const out = kWhat == kGram ? A : Q;
+    f16xN x[M];
+    if constexpr (kWhat == kPoly)
+#pragma unroll
+      for (uint32_t s = 0; s < M; s++) x[s] = *reinterpret_cast<const f16xN*>(A + uint64_t(i1 + 16 * s) * r.mp + j);
+    const float scale = kWhat == kGram ? kMuonLiftA / (r.lift * r.lift) : p.c * (1.0f / kMuonLiftA);
+#pragma unroll
+    for (uint32_t s = 0; s < M; s++) {
+      const uint32_t i = i1 + 16 * s;
+      f16xN h;
+#pragma unroll
+      for (uint32_t e = 0; e < 4 * N; e++) {
+        const float v = scale * acc[s][e / 4][e % 4];
+        h[e] = f16(kWhat == kPoly ? __builtin_fmaf(p.b, float(x[s][e]), v) : v);
+      }
+      *reinterpret_cast<f16xN*>(out + uint64_t(i) * r.mp + j) = h;
+      if (i0 != j0)
+#pragma unroll
+        for (uint32_t e = 0; e < 4 * N; e++) out[uint64_t(j + e) * r.mp + i] = h[e];
+    }
+  }
 }
 
 template <class T>
