@@ -173,20 +173,28 @@ __global__ __launch_bounds__(256) void k_muon_norm(MuonArgs a) {
 
 // ------------------------------------------------------------ X, as carried
 
-// X between steps: fp16, and where the next step wants it closer the rest in 8
-// bits, in 256ths of the fp16 number's last place, of which it is half at most.
-typedef int8_t i8x4 __attribute__((ext_vector_type(4)));
+// X between steps: fp16, and where the next step wants it closer the rest as an
+// 8-bit number (OCP e4m3) of 2^-kRestLift: four more bits of X down to 2^-12, where
+// an element is some 2^-6 of those that count.  Larger rests than it holds
+// belong to elements above 64, of which a matrix can have few.
+constexpr float kRestLift = 16384.0f, kMaxRest = 448.0f;
 
-__device__ __forceinline__ float last_place(f16 h) {
-  const uint32_t e = __builtin_bit_cast(uint16_t, h) >> 10 & 31;
-  return as_f(((e ? e : 1) + 127 - 25) << 23);
+// The numbers of four rests in a word, and the word of four values and their
+// fp16 numbers.
+__device__ __forceinline__ f32x4 rests(uint32_t w) {
+  const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+  return f32x4{lo[0], lo[1], hi[0], hi[1]};
 }
-__device__ __forceinline__ int8_t rest_of(float v, f16 h) {
-  const float q = __builtin_rintf((v - float(h)) * 256.0f / last_place(h));
-  return int8_t(__builtin_fminf(q, 127.0f));  // (NaN, of an infinity: any)
+__device__ __forceinline__ uint32_t rests_of(const f32x4& v, const f16x4& h) {
+  f32x4 q;
+#pragma unroll
+  for (int j = 0; j < 4; j++)  // (of an infinity or NaN: any)
+    q[j] = __builtin_amdgcn_fmed3f((v[j] - float(h[j])) * kRestLift, -kMaxRest, kMaxRest);
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
+  return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], w, true));
 }
-__device__ __forceinline__ float with_rest(f16 h, int8_t rest) {
-  return __builtin_fmaf(float(rest), last_place(h) * (1.0f / 256.0f), float(h));
+__device__ __forceinline__ float with_rest(f16 h, float rest) {
+  return __builtin_fmaf(rest, 1.0f / kRestLift, float(h));
 }
 
 // Four elements of a row of n from any element's address on, zeros behind them.
@@ -251,7 +259,7 @@ __global__ __launch_bounds__(256) void k_muon_spread(MuonArgs a) {
   const fr_muon_hyper h = a.hyper[r.group];
   const float scale = a.stats->scale;
   f16* const x = reinterpret_cast<f16*>(a.scratch + r.x[0]);
-  int8_t* const rest = reinterpret_cast<int8_t*>(a.scratch + r.rest);
+  uint8_t* const rest = a.scratch + r.rest;
   const uint32_t lo = threadIdx.x % 16 * 4, hi = threadIdx.x / 16;
   f32x4 v[4];
 #pragma unroll
@@ -275,15 +283,9 @@ __global__ __launch_bounds__(256) void k_muon_spread(MuonArgs a) {
 #pragma unroll
   for (uint32_t k = 0; k < 4; k++) {
     const uint64_t at = uint64_t(i0 + hi + 16 * k) * r.np + j0 + lo;
-    f16x4 y;
-    i8x4 z;
-#pragma unroll
-    for (uint32_t j = 0; j < 4; j++) {
-      y[j] = f16(v[k][j]);
-      z[j] = rest_of(v[k][j], y[j]);
-    }
+    const f16x4 y = __builtin_convertvector(v[k], f16x4);
     *reinterpret_cast<f16x4*>(x + at) = y;
-    *reinterpret_cast<i8x4*>(rest + at) = z;
+    *reinterpret_cast<uint32_t*>(rest + at) = rests_of(v[k], y);
   }
 }
 
@@ -304,16 +306,15 @@ struct ProductArgs {
   uint32_t last;
 };
 
-// How a workgroup makes a tile of B x B elements: waves of WM x WN, kStages slices
-// of the sum, kDeep deep, in LDS.
-template <uint32_t B_, uint32_t WM_, uint32_t WN_, uint32_t S_>
+// How a workgroup makes a tile of B x B elements: waves of WM x WN, S slices
+// of the sum, each D deep, in LDS.
+template <uint32_t B_, uint32_t WM_, uint32_t WN_, uint32_t S_, uint32_t D_>
 struct Shape {
-  static constexpr uint32_t B = B_, WM = WM_, WN = WN_, S = S_;
+  static constexpr uint32_t B = B_, WM = WM_, WN = WN_, S = S_, D = D_;
   static constexpr uint32_t waves = B / WM * (B / WN), threads = 64 * waves;
 };
-typedef Shape<256, 128, 64, 2> Large;
-typedef Shape<64, 32, 32, 4> Small;
-constexpr uint32_t kDeep = 64;
+typedef Shape<256, 128, 64, 2, 64> Large;
+typedef Shape<64, 32, 32, 4, 64> Small;
 
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
@@ -334,49 +335,48 @@ __device__ __forceinline__ void load_to_lds(const f16* base, uint32_t offset, co
 }
 
 // Which column of L R^T a lane of operand R stands for.  Of the 16 columns of a
-// matrix instruction's result a lane holds four in turn; the N of them that a
-// wave has side by side are interleaved, so that it holds 4 N in turn of a row.
-template <class T>
+// matrix instruction's result a lane holds four in turn; those of two are
+// interleaved, so that it holds 8 in turn of a row and four lanes 32.
 __device__ __forceinline__ uint32_t column_of(uint32_t q, uint32_t lane) {
-  return lane / 4 * (T::WN / 4) + q * 4 + lane % 4;
+  return q / 2 * 32 + lane / 4 * 8 + q % 2 * 4 + lane % 4;
 }
 
-// A slice of an operand whose rows run along the sum: B rows of kDeep.  Chunks of
+// A slice of an operand whose rows run along the sum: B rows of D.  Chunks of
 // 16 bytes are permuted by their row, so that the 16 rows whose chunk is read at
 // one time lie in different banks: rows in turn of L, column_of's of R.
 template <class T, bool kR>
 __device__ __forceinline__ uint32_t row_key(uint32_t row) {
-  return kR ? (row / 2 % 2) | row / (T::WN / 4) % 4 * 2 : row / 2 % 8;
+  if (T::D == 32) return kR ? row / 8 % 4 : row / 4 % 4;
+  return kR ? row / 2 % 2 | row / 8 % 4 * 2 : row / 2 % 8;
 }
 // (One offset a lane, of the first of a wave's loads: the others' rows have the
 // same keys, and the rest of their addresses is a scalar.)
 template <class T, bool kR>
 struct Rows {
+  static constexpr uint32_t kChunks = T::D / 8, kRows = 64 / kChunks;  // of a row, of a wave's load
   uint32_t offset;  // bytes
   __device__ __forceinline__ Rows(uint32_t wave, uint32_t ld) {
-    const uint32_t lane = threadIdx.x % 64, row = wave * 8 + lane / 8;
-    static_assert(T::waves * 8 % T::WN == 0, "keys of R go by rows mod WN");
-    offset = (row * ld + ((lane % 8) ^ row_key<T, kR>(row)) * 8) * 2;
+    const uint32_t lane = threadIdx.x % 64, row = wave * kRows + lane / kChunks;
+    static_assert(T::waves * kRows % 32 == 0, "keys go by rows mod 32");
+    offset = (row * ld + ((lane % kChunks) ^ row_key<T, kR>(row)) * 8) * 2;
   }
   __device__ __forceinline__ void fetch(const f16* src, uint32_t ld, f16* lds, uint32_t wave) const {
 #pragma unroll
-    for (uint32_t p = 0; p < T::B / 8 / T::waves; p++)
-      load_to_lds(src + uint64_t(p * T::waves * 8) * ld, offset, lds + (p * T::waves + wave) * 8 * kDeep);
+    for (uint32_t p = 0; p < T::B / kRows / T::waves; p++)
+      load_to_lds(src + uint64_t(p * T::waves * kRows) * ld, offset, lds + (p * T::waves + wave) * kRows * T::D);
   }
 };
 template <class T, bool kR>
 __device__ __forceinline__ f16x8 operand_of_row(const f16* lds, uint32_t row, uint32_t chunk) {
-  return *reinterpret_cast<const f16x8*>(lds + row * kDeep + (chunk ^ row_key<T, kR>(row)) * 8);
+  return *reinterpret_cast<const f16x8*>(lds + row * T::D + (chunk ^ row_key<T, kR>(row)) * 8);
 }
 
-// A slice of R where its columns run along the sum: kDeep rows of B.  Chunks are
+// A slice of R where its columns run along the sum: D rows of B.  Chunks are
 // permuted so that four columns of four rows each, as read at one time, lie in
 // different banks.
 template <class T>
 __device__ __forceinline__ uint32_t column_key(uint32_t row) {
-  constexpr uint32_t N = T::WN / 16;
-  static_assert((N == 4 && T::B == 256) || (N == 2 && T::B == 64), "the shapes there are");
-  return N == 4 ? (row & 1) | (row & 2) << 2 : (row & 2) << 1;
+  return T::B == 64 ? row / 2 % 2 * 4 : row % 4 * 4;
 }
 template <class T>
 struct Columns {
@@ -389,7 +389,7 @@ struct Columns {
   }
   __device__ __forceinline__ void fetch(const f16* src, uint32_t ld, f16* lds, uint32_t wave) const {
 #pragma unroll
-    for (uint32_t p = 0; p < kDeep / kRows / T::waves; p++)
+    for (uint32_t p = 0; p < T::D / kRows / T::waves; p++)
       load_to_lds(src + uint64_t(p * T::waves * kRows) * ld, offset, lds + (p * T::waves + wave) * kRows * T::B);
   }
 };
@@ -399,7 +399,7 @@ struct Columns {
 template <class T>
 __device__ __forceinline__ f16x8 operand_of_columns(const f16* lds, uint32_t col, uint32_t q, uint32_t kk) {
   const uint32_t lane = threadIdx.x % 64, quad = lane / 16, i = lane % 16;
-  const uint32_t c = col + column_of<T>(q, i % 4 * 4);
+  const uint32_t c = col + column_of(q, i % 4 * 4);
   union {
     f16x8 v;
     i16x4 half[2];
@@ -422,33 +422,36 @@ __device__ __forceinline__ void arrive() {
   asm volatile("" ::: "memory");
 }
 
-// A wave's operands of 32 of the sum: all N of R's, or half of the M of L's.
+// A wave's operands of 32 of the sum, those in use and those that are read ahead:
+// all N of R's, and halves of the M of L's.
 template <class T, bool kColumns>
 struct Operands {
   static constexpr uint32_t M = T::WM / 16, N = T::WN / 16, H = M / 2;
+  static constexpr uint32_t kReadsL = H, kReadsR = kColumns ? 2 * N : N;
   const uint32_t wi, wj;
   f16x8 y[2][N], x[2][H];
-  __device__ __forceinline__ void read_r(const f16* lds, uint32_t kk) {
+  // `kk`: which 32 of the slice
+  __device__ __forceinline__ void read_r(uint32_t set, const f16* lds, uint32_t kk) {
     const uint32_t lane = threadIdx.x % 64;
-    const f16* const r = lds + T::B * kDeep;
+    const f16* const r = lds + T::B * T::D;
 #pragma unroll
     for (uint32_t q = 0; q < N; q++)
-      y[kk][q] = kColumns ? operand_of_columns<T>(r, wj, q, kk)
-                          : operand_of_row<T, true>(r, wj + column_of<T>(q, lane % 16), kk * 4 + lane / 16);
+      y[set][q] = kColumns ? operand_of_columns<T>(r, wj, q, kk)
+                           : operand_of_row<T, true>(r, wj + column_of(q, lane % 16), kk * 4 + lane / 16);
   }
-  __device__ __forceinline__ void read_l(const f16* lds, uint32_t kk, uint32_t half) {
+  __device__ __forceinline__ void read_l(uint32_t half, const f16* lds, uint32_t kk) {
     const uint32_t lane = threadIdx.x % 64;
 #pragma unroll
     for (uint32_t s = 0; s < H; s++)
       x[half][s] = operand_of_row<T, false>(lds, wi + (half * H + s) * 16 + lane % 16, kk * 4 + lane / 16);
   }
-  __device__ __forceinline__ void multiply(f32x4 (&acc)[M][N], uint32_t kk, uint32_t half) const {
+  __device__ __forceinline__ void multiply(f32x4 (&acc)[M][N], uint32_t set, uint32_t half) const {
 #pragma unroll
     for (uint32_t s = 0; s < H; s++)
 #pragma unroll
       for (uint32_t q = 0; q < N; q++)
         acc[half * H + s][q] =
-            __builtin_amdgcn_mfma_f32_16x16x32_f16(y[kk][q], x[half][s], acc[half * H + s][q], 0, 0, 0);
+            __builtin_amdgcn_mfma_f32_16x16x32_f16(y[set][q], x[half][s], acc[half * H + s][q], 0, 0, 0);
   }
 };
 
@@ -471,7 +474,7 @@ template <Product kWhat, class T>
 __global__ __launch_bounds__(T::threads) void k_muon_product(ProductArgs p) {
   if (p.stats->nonfinite) return;
   extern __shared__ __attribute__((aligned(16))) f16 lds[];
-  constexpr uint32_t kSlice = T::B * kDeep, M = T::WM / 16, N = T::WN / 16;
+  constexpr uint32_t kSlice = T::B * T::D, M = T::WM / 16, N = T::WN / 16;
   constexpr uint32_t kLoads = 2 * kSlice / (8 * T::threads);  // of a wave, a slice of both operands
   const uint64_t tile = p.tiles[blockIdx.x];
   const MuonRec r = p.recs[tile >> 32];
@@ -486,116 +489,144 @@ __global__ __launch_bounds__(T::threads) void k_muon_product(ProductArgs p) {
   const f16* const pr = kWhat == kWhole ? X + j0 : (kWhat == kGram ? X : A) + uint64_t(j0) * K;
   const Rows<T, false> left(wave, K);
   const std::conditional_t<kWhat == kWhole, Columns<T>, Rows<T, true>> right(wave, kWhat == kWhole ? r.np : K);
-  const auto slice = [&](uint32_t k) { return lds + k / kDeep % T::S * 2 * kSlice; };
-  const auto fetch = [&](uint32_t k) {
-    left.fetch(pl + k, K, slice(k), wave);
-    if constexpr (kWhat == kWhole) right.fetch(pr + uint64_t(k) * r.np, r.np, slice(k) + kSlice, wave);
-    else right.fetch(pr + k, K, slice(k) + kSlice, wave);
-  };
   f32x4 acc[M][N] = {};
-  Operands<T, kWhat == kWhole> o{wi, wj};
-  // What is multiplied next is read while something else is: halves of L's rows,
-  // and R's columns for the next 32 of the sum.
-  const auto first_three = [&](const f16* from) {
-    o.read_l(from, 0, 1);
-    o.read_r(from, 1);
-    o.multiply(acc, 0, 0);
-    interleave<M / 2 + (kWhat == kWhole ? 2 : 1) * N, M * N / 2>();
-    o.read_l(from, 1, 0);
-    o.multiply(acc, 0, 1);
-    interleave<M / 2, M * N / 2>();
-    o.read_l(from, 1, 1);
-    o.multiply(acc, 1, 0);
-    interleave<M / 2, M * N / 2>();
+  typedef Operands<T, kWhat == kWhole> Ops;
+  Ops o{wi, wj};
+  // Slices lie in a ring: `at` is read, `free` loaded next.
+  const f16* at = lds;
+  f16* free = lds;
+  const auto following = [&](auto* x) { return x == lds + (T::S - 1) * 2 * kSlice ? x - (T::S - 1) * 2 * kSlice : x + 2 * kSlice; };
+  const auto fetch = [&](uint32_t k) {
+    left.fetch(pl + k, K, free, wave);
+    if constexpr (kWhat == kWhole) right.fetch(pr + uint64_t(k) * r.np, r.np, free + kSlice, wave);
+    else right.fetch(pr + k, K, free + kSlice, wave);
+    free = following(free);
   };
-  const auto last_one = [&](const f16* next) {
-    o.read_r(next, 0);
-    o.read_l(next, 0, 0);
-    o.multiply(acc, 1, 1);
-    interleave<M / 2 + (kWhat == kWhole ? 2 : 1) * N, M * N / 2>();
+  // What is multiplied next is read while something else is.  The first half of
+  // 32 of the sum:
+  const auto first_half = [&](uint32_t set, uint32_t kk) {
+    o.read_l(1, at, kk);
+    o.multiply(acc, set, 0);
+    interleave<Ops::kReadsL, M * N / 2>();
+  };
+  // and the second, with what the next 32 begin with.
+  const auto second_half = [&](uint32_t set, uint32_t kk) {
+    o.read_r(set ^ 1, at, kk);
+    o.read_l(0, at, kk);
+    o.multiply(acc, set, 1);
+    interleave<Ops::kReadsL + Ops::kReadsR, M * N / 2>();
   };
 #pragma unroll
   for (uint32_t s = 0; s < T::S; s++)
-    if (s * kDeep < K) fetch(s * kDeep);
-  if (T::S * kDeep <= K) arrive<(T::S - 1) * kLoads>();
+    if (s * T::D < K) fetch(s * T::D);
+  if (T::S * T::D <= K) arrive<(T::S - 1) * kLoads>();
   else arrive<0>();
-  o.read_r(slice(0), 0);
-  o.read_l(slice(0), 0, 0);
+  o.read_r(0, at, 0);
+  o.read_l(0, at, 0);
+  // 64 of the sum, one slice or two, after each of which there may be another to
+  // load (where there is none, the waits are for all)
+  const auto sixty_four = [&](uint32_t k, auto first, auto second, auto last) {
+    const auto next_slice = [&](uint32_t load, auto more) {
+      // the next slice is there, and nobody reads this one any more
+      if constexpr (more) {
+        arrive<(T::S - 2) * kLoads>();
+        fetch(load);
+      } else {
+        arrive<0>();
+      }
+      at = following(at);
+    };
+    first_half(0, 0);
+    if constexpr (T::D == 32) {
+      next_slice(k + T::S * 32, first);
+      second_half(0, 0);
+    } else {
+      second_half(0, 1);
+    }
+    first_half(1, T::D == 32 ? 0 : 1);
+    if constexpr (last) {
+      o.multiply(acc, 1, 1);
+    } else {
+      next_slice(k + 64 - T::D + T::S * T::D, second);
+      second_half(1, 0);
+    }
+  };
+  constexpr std::true_type yes;
+  constexpr std::false_type no;
   uint32_t k = 0;
-  for (; k + T::S * kDeep < K; k += kDeep) {
-    first_three(slice(k));
-    arrive<(T::S - 2) * kLoads>();  // the next slice is there, and nobody reads this one any more
-    fetch(k + T::S * kDeep);
-    last_one(slice(k + kDeep));
+  for (; k + 64 - T::D + T::S * T::D < K; k += 64) sixty_four(k, yes, yes, no);
+  if constexpr (T::D == 32 && T::S % 2 == 1) {
+    if (k + T::S * T::D < K) {
+      sixty_four(k, yes, no, no);
+      k += 64;
+    }
   }
-  for (; k + kDeep < K; k += kDeep) {  // nothing is left to load: waits for all
-    first_three(slice(k));
-    arrive<0>();
-    last_one(slice(k + kDeep));
-  }
-  first_three(slice(k));
-  o.multiply(acc, 1, 1);
+  for (; k + 64 < K; k += 64) sixty_four(k, no, no, no);
+  sixty_four(k, no, no, yes);
 
-  // of rows wi + 16 s + lane % 16 a lane holds 4 N columns in turn
+  // of rows wi + 16 s + lane % 16 a lane holds 8 columns in turn for each two of N
   f16* const to = reinterpret_cast<f16*>(p.scratch + (p.flip ? r.x[0] : r.x[1]));
-  int8_t* const rest = reinterpret_cast<int8_t*>(p.scratch + r.rest);
-  const uint32_t i1 = i0 + wi + lane % 16, j = j0 + wj + lane / 16 * 4 * N;
-  typedef f16 f16xN __attribute__((ext_vector_type(4 * N)));
-  typedef int8_t i8xN __attribute__((ext_vector_type(4 * N)));
+  uint8_t* const rest = p.scratch + r.rest;
+  const uint32_t i1 = i0 + wi + lane % 16, j1 = j0 + wj + lane / 16 * 8;
   if constexpr (kWhat == kWhole) {
     const auto finish = [&](auto carried, auto carry, auto last) {
       constexpr uint32_t G = M < 4 ? M : 4;  // rows' loads in flight together
-      f16xN x[G];
-      i8xN z[G];
+      f16x8 x[G][N / 2];
+      u32x2 z[G][N / 2];
 #pragma unroll
       for (uint32_t s = 0; s < M; s++) {
-        const uint32_t i = i1 + 16 * s, g = s % G;
-        const uint64_t at = uint64_t(i) * r.np + j;
-        if (g == 0) {
+        const uint32_t i = i1 + 16 * s;
+        if (s % G == 0) {
           __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (uint32_t n = 0; n < G; n++) {
-            x[n] = *reinterpret_cast<const f16xN*>(X + at + uint64_t(16 * n) * r.np);
-            if constexpr (carried) z[n] = *reinterpret_cast<const i8xN*>(rest + at + uint64_t(16 * n) * r.np);
+          for (uint32_t n = 0; n < G; n++)
+#pragma unroll
+            for (uint32_t c = 0; c < N / 2; c++) {
+              const uint64_t at = uint64_t(i + 16 * n) * r.np + j1 + 32 * c;
+              x[n][c] = *reinterpret_cast<const f16x8*>(X + at);
+              if constexpr (carried) z[n][c] = *reinterpret_cast<const u32x2*>(rest + at);
+            }
+        }
+#pragma unroll
+        for (uint32_t c = 0; c < N / 2; c++) {
+          const uint32_t j = j1 + 32 * c;
+          const uint64_t at = uint64_t(i) * r.np + j;
+          f32x4 v[2];
+          f16x4 h[2];
+          u32x2 w;
+#pragma unroll
+          for (uint32_t k = 0; k < 2; k++) {
+            f32x4 more = {0, 0, 0, 0};
+            if constexpr (carried) more = rests(z[s % G][c][k]);
+#pragma unroll
+            for (uint32_t e = 0; e < 4; e++) {
+              const f16 was = x[s % G][c][4 * k + e];
+              v[k][e] = __builtin_fmaf(p.a, carried ? with_rest(was, more[e]) : float(was),
+                                       acc[s][2 * c + k][e] * (1.0f / kMuonLiftA));
+            }
+            h[k] = __builtin_convertvector(v[k], f16x4);
+            if constexpr (carry) w[k] = rests_of(v[k], h[k]);
           }
-        }
-        float v[4 * N];
-        f16xN h;
+          if constexpr (!last) {
+            *reinterpret_cast<f16x8*>(to + at) = __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7);
+            if constexpr (carry) *reinterpret_cast<u32x2*>(rest + at) = w;
+          } else if (i < r.m && j < r.n) {
+            uint16_t* const out = reinterpret_cast<uint16_t*>(p.updates + r.update);
+            const float down = 1.0f / r.lift;
+            if (r.wide && r.cols % 8 == 0) {
+              const u32x2 lo = to_bf16(v[0] * down), hi = to_bf16(v[1] * down);
+              *reinterpret_cast<u32x4*>(out + uint64_t(i) * r.cols + j) = u32x4{lo.x, lo.y, hi.x, hi.y};
+            } else {
 #pragma unroll
-        for (uint32_t e = 0; e < 4 * N; e++) {
-          float was;
-          if constexpr (carried) was = with_rest(x[g][e], z[g][e]);
-          else was = float(x[g][e]);
-          v[e] = __builtin_fmaf(p.a, was, acc[s][e / 4][e % 4] * (1.0f / kMuonLiftA));
-          h[e] = f16(v[e]);
-          if constexpr (carry) z[g][e] = rest_of(v[e], h[e]);
-        }
-        if constexpr (!last) {
-          *reinterpret_cast<f16xN*>(to + at) = h;
-          if constexpr (carry) *reinterpret_cast<i8xN*>(rest + at) = z[g];
-        } else if (i < r.m && j < r.n) {
-          uint16_t* const out = reinterpret_cast<uint16_t*>(p.updates + r.update);
-          const float down = 1.0f / r.lift;
-          if (r.wide && r.cols % 8 == 0) {
-#pragma unroll
-            for (uint32_t e = 0; e < 4 * N; e += 8)
-              if (j + e < r.n) {
-                const u32x2 lo = to_bf16(f32x4{v[e] * down, v[e + 1] * down, v[e + 2] * down, v[e + 3] * down});
-                const u32x2 hi = to_bf16(f32x4{v[e + 4] * down, v[e + 5] * down, v[e + 6] * down, v[e + 7] * down});
-                *reinterpret_cast<u32x4*>(out + uint64_t(i) * r.cols + j + e) = u32x4{lo.x, lo.y, hi.x, hi.y};
-              }
-          } else {
-#pragma unroll
-            for (uint32_t e = 0; e < 4 * N; e++)
-              if (j + e < r.n)
-                out[r.wide ? uint64_t(i) * r.cols + j + e : uint64_t(j + e) * r.cols + i] =
-                    uint16_t(rne_bf16(as_u(v[e] * down)));
+              for (uint32_t e = 0; e < 8; e++)
+                if (j + e < r.n)
+                  out[r.wide ? uint64_t(i) * r.cols + j + e : uint64_t(j + e) * r.cols + i] =
+                      uint16_t(rne_bf16(as_u(v[e / 4][e % 4] * down)));
+            }
           }
         }
       }
     };
-    constexpr std::true_type yes;
-    constexpr std::false_type no;
     if (p.last) {
       if (p.carried) finish(yes, no, yes);
       else finish(no, no, yes);
@@ -608,31 +639,59 @@ __global__ __launch_bounds__(T::threads) void k_muon_product(ProductArgs p) {
     }
   } else {
     f16* const out = kWhat == kGram ? A : Q;
-    f16xN x[M];
+    const float scale = kWhat == kGram ? kMuonLiftA / (r.lift * r.lift) : p.c * (1.0f / kMuonLiftA);
+    f16x8 x[M][N / 2];
     if constexpr (kWhat == kPoly)
 #pragma unroll
-      for (uint32_t s = 0; s < M; s++) x[s] = *reinterpret_cast<const f16xN*>(A + uint64_t(i1 + 16 * s) * r.mp + j);
-    const float scale = kWhat == kGram ? kMuonLiftA / (r.lift * r.lift) : p.c * (1.0f / kMuonLiftA);
+      for (uint32_t s = 0; s < M; s++)
 #pragma unroll
-    for (uint32_t s = 0; s < M; s++) {
-      const uint32_t i = i1 + 16 * s;
-      f16xN h;
+        for (uint32_t c = 0; c < N / 2; c++)
+          x[s][c] = *reinterpret_cast<const f16x8*>(A + uint64_t(i1 + 16 * s) * r.mp + j1 + 32 * c);
+    // The tile's mirror image goes by way of LDS, each wave's part by itself: rows
+    // of WN, whose chunks of 16 bytes are permuted by their row, and transposing
+    // reads, which give a lane eight rows of its column.
+    constexpr uint32_t kChunks = T::WN / 8;
+    f16* const mirror = lds + wave * (T::WM * T::WN);
+    arrive<0>();
 #pragma unroll
-      for (uint32_t e = 0; e < 4 * N; e++) {
-        const float v = scale * acc[s][e / 4][e % 4];
-        h[e] = f16(kWhat == kPoly ? __builtin_fmaf(p.b, float(x[s][e]), v) : v);
+    for (uint32_t s = 0; s < M; s++)
+#pragma unroll
+      for (uint32_t c = 0; c < N / 2; c++) {
+        f16x8 h;
+#pragma unroll
+        for (uint32_t e = 0; e < 8; e++) {
+          const float v = scale * acc[s][2 * c + e / 4][e % 4];
+          h[e] = f16(kWhat == kPoly ? __builtin_fmaf(p.b, float(x[s][c][e]), v) : v);
+        }
+        *reinterpret_cast<f16x8*>(out + uint64_t(i1 + 16 * s) * r.mp + j1 + 32 * c) = h;
+        const uint32_t row = s * 16 + lane % 16, chunk = c * 4 + lane / 16;
+        *reinterpret_cast<f16x8*>(mirror + row * T::WN + (chunk ^ (row / 2 % kChunks)) * 8) = h;
       }
-      *reinterpret_cast<f16xN*>(out + uint64_t(i) * r.mp + j) = h;
-      if (i0 != j0)
+    if (i0 == j0) return;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (of this wave's own writes)
 #pragma unroll
-        for (uint32_t e = 0; e < 4 * N; e++) out[uint64_t(j + e) * r.mp + i] = h[e];
-    }
+    for (uint32_t b = 0; b < T::WM / 32; b++)
+#pragma unroll
+      for (uint32_t q = 0; q < N; q++) {
+        const uint32_t row = b * 32 + lane / 16 * 8, column = q * 16 + lane % 4 * 4;
+        union {
+          f16x8 v;
+          i16x4 half[2];
+        } u;
+#pragma unroll
+        for (uint32_t h = 0; h < 2; h++) {
+          const uint32_t k = row + 4 * h + lane % 16 / 4;
+          u.half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (lds_i16x4*)(mirror + k * T::WN + ((column / 8) ^ (k / 2 % kChunks)) * 8 + column % 8));
+        }
+        *reinterpret_cast<f16x8*>(out + uint64_t(j0 + wj + q * 16 + lane % 16) * r.mp + i0 + wi + row) = u.v;
+      }
   }
 }
 
 template <class T>
 int products(const MuonArgs& a, hipStream_t st) {
-  constexpr uint32_t lds = T::S * 2 * T::B * kDeep * sizeof(f16);
+  constexpr uint32_t lds = T::S * 2 * T::B * T::D * sizeof(f16);
   for (uint32_t s = 0; s < a.n_steps; s++) {
     ProductArgs p;
     p.recs = a.recs;
