@@ -312,7 +312,11 @@ int build(fr_muon* o) {
   const hipError_t es = hipStreamSynchronize(s);
   (void)hipStreamDestroy(s);
   if (e != hipSuccess || es != hipSuccess) return device_error(e != hipSuccess ? e : es);
+  int units = 0;
+  e = hipDeviceGetAttribute(&units, hipDeviceAttributeMultiprocessorCount, o->device);
+  if (e != hipSuccess) return device_error(e);
   MuonArgs& a = o->args;
+  a.units = uint32_t(units);
   a.recs = reinterpret_cast<const MuonRec*>(at(recs));
   a.n = n;
   a.side = Y.side;

@@ -45,6 +45,7 @@ struct MuonArgs {
   const MuonRec* recs = nullptr;
   uint32_t n = 0;
   uint32_t side = kMuonSmall;  // of the products' tiles
+  uint32_t units = 1;          // compute units, each of which takes one workgroup of large tiles
   AdamwWalk walk;          // tiles of kMuonTile elements
   uint8_t* scratch = nullptr;
   double* parts = nullptr;  // a sum of squares for each place of the walk

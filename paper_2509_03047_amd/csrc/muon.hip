@@ -189,12 +189,9 @@ __device__ __forceinline__ uint32_t rests_of(const f32x4& v, const f16x4& h) {
   f32x4 q;
 #pragma unroll
   for (int j = 0; j < 4; j++)  // (of an infinity or NaN: any)
-    q[j] = __builtin_amdgcn_fmed3f((v[j] - float(h[j])) * kRestLift, -kMaxRest, kMaxRest);
+    q[j] = __builtin_amdgcn_fmed3f(__builtin_fmaf(float(h[j]), -kRestLift, v[j] * kRestLift), -kMaxRest, kMaxRest);
   int w = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
   return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], w, true));
-}
-__device__ __forceinline__ float with_rest(f16 h, float rest) {
-  return __builtin_fmaf(rest, 1.0f / kRestLift, float(h));
 }
 
 // Four elements of a row of n from any element's address on, zeros behind them.
@@ -291,11 +288,12 @@ __global__ __launch_bounds__(256) void k_muon_spread(MuonArgs a) {
 
 // ------------------------------------------------------------------ products
 
-enum Product { kGram, kPoly, kWhole };
+enum MuonProduct { kGram, kPoly, kWhole };
 
 struct ProductArgs {
   const MuonRec* recs;
   const uint64_t* tiles;
+  uint32_t n;  // tiles
   uint8_t* scratch;
   uint8_t* updates;
   const fr_grad_stats* stats;
@@ -469,27 +467,49 @@ __device__ __forceinline__ void interleave() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// One tile of L R (kWhole, with R's columns along the sum) or L R^T.
-template <Product kWhat, class T>
+// LDS of a workgroup: the ring of slices, and behind it 32 rows of each wave's
+// results on their way to the other side of the diagonal.
+template <class T>
+struct Lds {
+  static constexpr uint32_t slice = T::B * T::D;  // of one operand
+  static constexpr uint32_t ring = T::S * 2 * slice, mirror = 32 * T::WN;
+  static constexpr uint32_t bytes = (ring + T::waves * mirror) * sizeof(f16);
+};
+
+// What a workgroup needs to know of a tile to load and multiply.
+template <MuonProduct kWhat, class T>
+struct Place {
+  const MuonRec* rec;
+  uint32_t i0, j0, K, ld;  // ld: of R's rows
+  const f16 *pl, *pr;
+  Rows<T, false> left;
+  std::conditional_t<kWhat == kWhole, Columns<T>, Rows<T, true>> right;
+  static __device__ __forceinline__ Place of(const ProductArgs& p, uint32_t t, uint32_t wave) {
+    const uint64_t tile = p.tiles[t];
+    const MuonRec* const rec = p.recs + (tile >> 32);
+    const uint32_t i0 = uint32_t(tile >> 16 & 0xFFFF) * T::B, j0 = uint32_t(tile & 0xFFFF) * T::B;
+    const uint32_t K = kWhat == kGram ? rec->np : rec->mp, ld = kWhat == kWhole ? rec->np : K;
+    const f16* const X = reinterpret_cast<const f16*>(p.scratch + rec->x[p.flip]);
+    const f16* const A = reinterpret_cast<const f16*>(p.scratch + rec->a);
+    const f16* const L = kWhat == kGram ? X : kWhat == kPoly ? A : reinterpret_cast<const f16*>(p.scratch + rec->q);
+    return Place{rec, i0, j0, K, ld, L + uint64_t(i0) * K,
+                 kWhat == kWhole ? X + j0 : (kWhat == kGram ? X : A) + uint64_t(j0) * K, {wave, K}, {wave, ld}};
+  }
+};
+
+// Tiles of L R (kWhole, with R's columns along the sum) or L R^T, one after
+// another: the next one's first slices are loaded while one's results are stored.
+template <MuonProduct kWhat, class T>
 __global__ __launch_bounds__(T::threads) void k_muon_product(ProductArgs p) {
   if (p.stats->nonfinite) return;
   extern __shared__ __attribute__((aligned(16))) f16 lds[];
-  constexpr uint32_t kSlice = T::B * T::D, M = T::WM / 16, N = T::WN / 16;
+  constexpr uint32_t kSlice = Lds<T>::slice, M = T::WM / 16, N = T::WN / 16;
   constexpr uint32_t kLoads = 2 * kSlice / (8 * T::threads);  // of a wave, a slice of both operands
-  const uint64_t tile = p.tiles[blockIdx.x];
-  const MuonRec r = p.recs[tile >> 32];
-  const uint32_t i0 = uint32_t(tile >> 16 & 0xFFFF) * T::B, j0 = uint32_t(tile & 0xFFFF) * T::B;
-  f16* const X = reinterpret_cast<f16*>(p.scratch + (p.flip ? r.x[1] : r.x[0]));
-  f16* const A = reinterpret_cast<f16*>(p.scratch + r.a);
-  f16* const Q = reinterpret_cast<f16*>(p.scratch + r.q);
-  const uint32_t K = kWhat == kGram ? r.np : r.mp;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
   const uint32_t wi = wave / (T::B / T::WN) * T::WM, wj = wave % (T::B / T::WN) * T::WN;
-  const f16* const pl = (kWhat == kGram ? X : kWhat == kPoly ? A : Q) + uint64_t(i0) * K;
-  const f16* const pr = kWhat == kWhole ? X + j0 : (kWhat == kGram ? X : A) + uint64_t(j0) * K;
-  const Rows<T, false> left(wave, K);
-  const std::conditional_t<kWhat == kWhole, Columns<T>, Rows<T, true>> right(wave, kWhat == kWhole ? r.np : K);
-  f32x4 acc[M][N] = {};
+  typedef Place<kWhat, T> Here;
+  Here here = Here::of(p, blockIdx.x, wave);
+  f32x4 acc[M][N];
   typedef Operands<T, kWhat == kWhole> Ops;
   Ops o{wi, wj};
   // Slices lie in a ring: `at` is read, `free` loaded next.
@@ -497,10 +517,16 @@ __global__ __launch_bounds__(T::threads) void k_muon_product(ProductArgs p) {
   f16* free = lds;
   const auto following = [&](auto* x) { return x == lds + (T::S - 1) * 2 * kSlice ? x - (T::S - 1) * 2 * kSlice : x + 2 * kSlice; };
   const auto fetch = [&](uint32_t k) {
-    left.fetch(pl + k, K, free, wave);
-    if constexpr (kWhat == kWhole) right.fetch(pr + uint64_t(k) * r.np, r.np, free + kSlice, wave);
-    else right.fetch(pr + k, K, free + kSlice, wave);
+    here.left.fetch(here.pl + k, here.K, free, wave);
+    if constexpr (kWhat == kWhole) here.right.fetch(here.pr + uint64_t(k) * here.ld, here.ld, free + kSlice, wave);
+    else here.right.fetch(here.pr + k, here.ld, free + kSlice, wave);
     free = following(free);
+  };
+  const auto fetch_first = [&] {
+    at = free = lds;
+#pragma unroll
+    for (uint32_t s = 0; s < T::S; s++)
+      if (s * T::D < here.K) fetch(s * T::D);
   };
   // What is multiplied next is read while something else is.  The first half of
   // 32 of the sum:
@@ -516,13 +542,6 @@ __global__ __launch_bounds__(T::threads) void k_muon_product(ProductArgs p) {
     o.multiply(acc, set, 1);
     interleave<Ops::kReadsL + Ops::kReadsR, M * N / 2>();
   };
-#pragma unroll
-  for (uint32_t s = 0; s < T::S; s++)
-    if (s * T::D < K) fetch(s * T::D);
-  if (T::S * T::D <= K) arrive<(T::S - 1) * kLoads>();
-  else arrive<0>();
-  o.read_r(0, at, 0);
-  o.read_l(0, at, 0);
   // 64 of the sum, one slice or two, after each of which there may be another to
   // load (where there is none, the waits are for all)
   const auto sixty_four = [&](uint32_t k, auto first, auto second, auto last) {
@@ -553,145 +572,177 @@ __global__ __launch_bounds__(T::threads) void k_muon_product(ProductArgs p) {
   };
   constexpr std::true_type yes;
   constexpr std::false_type no;
-  uint32_t k = 0;
-  for (; k + 64 - T::D + T::S * T::D < K; k += 64) sixty_four(k, yes, yes, no);
-  if constexpr (T::D == 32 && T::S % 2 == 1) {
-    if (k + T::S * T::D < K) {
-      sixty_four(k, yes, no, no);
-      k += 64;
-    }
-  }
-  for (; k + 64 < K; k += 64) sixty_four(k, no, no, no);
-  sixty_four(k, no, no, yes);
 
-  // of rows wi + 16 s + lane % 16 a lane holds 8 columns in turn for each two of N
-  f16* const to = reinterpret_cast<f16*>(p.scratch + (p.flip ? r.x[0] : r.x[1]));
-  uint8_t* const rest = p.scratch + r.rest;
-  const uint32_t i1 = i0 + wi + lane % 16, j1 = j0 + wj + lane / 16 * 8;
-  if constexpr (kWhat == kWhole) {
-    const auto finish = [&](auto carried, auto carry, auto last) {
-      constexpr uint32_t G = M < 4 ? M : 4;  // rows' loads in flight together
-      f16x8 x[G][N / 2];
-      u32x2 z[G][N / 2];
-#pragma unroll
-      for (uint32_t s = 0; s < M; s++) {
-        const uint32_t i = i1 + 16 * s;
-        if (s % G == 0) {
-          __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-          for (uint32_t n = 0; n < G; n++)
-#pragma unroll
-            for (uint32_t c = 0; c < N / 2; c++) {
-              const uint64_t at = uint64_t(i + 16 * n) * r.np + j1 + 32 * c;
-              x[n][c] = *reinterpret_cast<const f16x8*>(X + at);
-              if constexpr (carried) z[n][c] = *reinterpret_cast<const u32x2*>(rest + at);
-            }
-        }
-#pragma unroll
-        for (uint32_t c = 0; c < N / 2; c++) {
-          const uint32_t j = j1 + 32 * c;
-          const uint64_t at = uint64_t(i) * r.np + j;
-          f32x4 v[2];
-          f16x4 h[2];
-          u32x2 w;
-#pragma unroll
-          for (uint32_t k = 0; k < 2; k++) {
-            f32x4 more = {0, 0, 0, 0};
-            if constexpr (carried) more = rests(z[s % G][c][k]);
-#pragma unroll
-            for (uint32_t e = 0; e < 4; e++) {
-              const f16 was = x[s % G][c][4 * k + e];
-              v[k][e] = __builtin_fmaf(p.a, carried ? with_rest(was, more[e]) : float(was),
-                                       acc[s][2 * c + k][e] * (1.0f / kMuonLiftA));
-            }
-            h[k] = __builtin_convertvector(v[k], f16x4);
-            if constexpr (carry) w[k] = rests_of(v[k], h[k]);
-          }
-          if constexpr (!last) {
-            *reinterpret_cast<f16x8*>(to + at) = __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7);
-            if constexpr (carry) *reinterpret_cast<u32x2*>(rest + at) = w;
-          } else if (i < r.m && j < r.n) {
-            uint16_t* const out = reinterpret_cast<uint16_t*>(p.updates + r.update);
-            const float down = 1.0f / r.lift;
-            if (r.wide && r.cols % 8 == 0) {
-              const u32x2 lo = to_bf16(v[0] * down), hi = to_bf16(v[1] * down);
-              *reinterpret_cast<u32x4*>(out + uint64_t(i) * r.cols + j) = u32x4{lo.x, lo.y, hi.x, hi.y};
-            } else {
-#pragma unroll
-              for (uint32_t e = 0; e < 8; e++)
-                if (j + e < r.n)
-                  out[r.wide ? uint64_t(i) * r.cols + j + e : uint64_t(j + e) * r.cols + i] =
-                      uint16_t(rne_bf16(as_u(v[e / 4][e % 4] * down)));
-            }
-          }
-        }
-      }
-    };
-    if (p.last) {
-      if (p.carried) finish(yes, no, yes);
-      else finish(no, no, yes);
-    } else if (p.carry) {
-      finish(yes, yes, no);
-    } else if (p.carried) {
-      finish(yes, no, no);
-    } else {
-      finish(no, no, no);
-    }
-  } else {
-    f16* const out = kWhat == kGram ? A : Q;
-    const float scale = kWhat == kGram ? kMuonLiftA / (r.lift * r.lift) : p.c * (1.0f / kMuonLiftA);
-    f16x8 x[M][N / 2];
-    if constexpr (kWhat == kPoly)
+  fetch_first();
+  for (uint32_t t = blockIdx.x;;) {
+    // of rows i1 + 16 s a lane holds 8 columns in turn, from j1 + 32 c on
+    uint32_t i1 = here.i0 + wi + lane % 16, j1 = here.j0 + wj + lane / 16 * 8;
+    // The sums start from what X itself contributes, as far as a product is stored
+    // times kMuonLiftA.
+    if constexpr (kWhat == kWhole) {
+      const f16* const X = reinterpret_cast<const f16*>(p.scratch + here.rec->x[p.flip]);
+      const float a = p.a * kMuonLiftA, b = a / kRestLift;
+      f16x8 x[M][N / 2];
 #pragma unroll
       for (uint32_t s = 0; s < M; s++)
 #pragma unroll
         for (uint32_t c = 0; c < N / 2; c++)
-          x[s][c] = *reinterpret_cast<const f16x8*>(A + uint64_t(i1 + 16 * s) * r.mp + j1 + 32 * c);
-    // The tile's mirror image goes by way of LDS, each wave's part by itself: rows
-    // of WN, whose chunks of 16 bytes are permuted by their row, and transposing
-    // reads, which give a lane eight rows of its column.
-    constexpr uint32_t kChunks = T::WN / 8;
-    f16* const mirror = lds + wave * (T::WM * T::WN);
-    arrive<0>();
+          x[s][c] = *reinterpret_cast<const f16x8*>(X + uint64_t(i1 + 16 * s) * here.ld + j1 + 32 * c);
+      if (p.carried) {
+        const uint8_t* const rest = p.scratch + here.rec->rest;
+        u32x2 z[M][N / 2];
 #pragma unroll
-    for (uint32_t s = 0; s < M; s++)
+        for (uint32_t s = 0; s < M; s++)
 #pragma unroll
-      for (uint32_t c = 0; c < N / 2; c++) {
-        f16x8 h;
+          for (uint32_t c = 0; c < N / 2; c++)
+            z[s][c] = *reinterpret_cast<const u32x2*>(rest + uint64_t(i1 + 16 * s) * here.ld + j1 + 32 * c);
 #pragma unroll
-        for (uint32_t e = 0; e < 8; e++) {
-          const float v = scale * acc[s][2 * c + e / 4][e % 4];
-          h[e] = f16(kWhat == kPoly ? __builtin_fmaf(p.b, float(x[s][c][e]), v) : v);
-        }
-        *reinterpret_cast<f16x8*>(out + uint64_t(i1 + 16 * s) * r.mp + j1 + 32 * c) = h;
-        const uint32_t row = s * 16 + lane % 16, chunk = c * 4 + lane / 16;
-        *reinterpret_cast<f16x8*>(mirror + row * T::WN + (chunk ^ (row / 2 % kChunks)) * 8) = h;
+        for (uint32_t s = 0; s < M; s++)
+#pragma unroll
+          for (uint32_t q = 0; q < N; q++) {
+            const f32x4 more = rests(z[s][q / 2][q % 2]);
+#pragma unroll
+            for (uint32_t e = 0; e < 4; e++)
+              acc[s][q][e] = __builtin_fmaf(float(x[s][q / 2][q % 2 * 4 + e]), a, more[e] * b);
+          }
+      } else {
+#pragma unroll
+        for (uint32_t s = 0; s < M; s++)
+#pragma unroll
+          for (uint32_t q = 0; q < N; q++)
+#pragma unroll
+            for (uint32_t e = 0; e < 4; e++) acc[s][q][e] = a * float(x[s][q / 2][q % 2 * 4 + e]);
       }
-    if (i0 == j0) return;
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (of this wave's own writes)
+    } else {
 #pragma unroll
-    for (uint32_t b = 0; b < T::WM / 32; b++)
+      for (uint32_t s = 0; s < M; s++)
 #pragma unroll
-      for (uint32_t q = 0; q < N; q++) {
-        const uint32_t row = b * 32 + lane / 16 * 8, column = q * 16 + lane % 4 * 4;
-        union {
-          f16x8 v;
-          i16x4 half[2];
-        } u;
-#pragma unroll
-        for (uint32_t h = 0; h < 2; h++) {
-          const uint32_t k = row + 4 * h + lane % 16 / 4;
-          u.half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (lds_i16x4*)(mirror + k * T::WN + ((column / 8) ^ (k / 2 % kChunks)) * 8 + column % 8));
-        }
-        *reinterpret_cast<f16x8*>(out + uint64_t(j0 + wj + q * 16 + lane % 16) * r.mp + i0 + wi + row) = u.v;
+        for (uint32_t q = 0; q < N; q++) acc[s][q] = f32x4{0, 0, 0, 0};
+    }
+    const uint32_t K = here.K;
+    if (T::S * T::D <= K) arrive<(T::S - 1) * kLoads>();
+    else arrive<0>();
+    o.read_r(0, at, 0);
+    o.read_l(0, at, 0);
+    uint32_t k = 0;
+    for (; k + 64 - T::D + T::S * T::D < K; k += 64) sixty_four(k, yes, yes, no);
+    if constexpr (T::D == 32 && T::S % 2 == 1) {
+      if (k + T::S * T::D < K) {
+        sixty_four(k, yes, no, no);
+        k += 64;
       }
+    }
+    for (; k + 64 < K; k += 64) sixty_four(k, no, no, no);
+    sixty_four(k, no, no, yes);
+
+    const MuonRec* const rec = here.rec;
+    const bool diagonal = here.i0 == here.j0;
+    const uint32_t i2 = here.j0 + wj + lane % 16, j2 = here.i0 + wi + lane / 16 * 8;  // of the mirror image
+    t += gridDim.x;
+    const bool more = t < p.n;
+    if (more) {
+      here = Here::of(p, t, wave);
+      arrive<0>();  // nobody reads the ring any more
+      fetch_first();
+    }
+    if constexpr (kWhat == kWhole) {
+      const MuonRec& r = *rec;
+      f16* const to = reinterpret_cast<f16*>(p.scratch + r.x[p.flip ^ 1]);
+      uint8_t* const rest = p.scratch + r.rest;
+      const float down = (p.last ? 1.0f / r.lift : 1.0f) / kMuonLiftA;
+      const auto finish = [&](auto carry, auto last) {
+#pragma unroll
+        for (uint32_t s = 0; s < M; s++) {
+          const uint32_t i = i1 + 16 * s;
+#pragma unroll
+          for (uint32_t c = 0; c < N / 2; c++) {
+            const uint32_t j = j1 + 32 * c;
+            const uint64_t to_at = uint64_t(i) * r.np + j;
+            const f32x4 v[2] = {acc[s][2 * c] * down, acc[s][2 * c + 1] * down};
+            if constexpr (!last) {
+              const f16x4 h[2] = {__builtin_convertvector(v[0], f16x4), __builtin_convertvector(v[1], f16x4)};
+              *reinterpret_cast<f16x8*>(to + to_at) = __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7);
+              if constexpr (carry)
+                *reinterpret_cast<u32x2*>(rest + to_at) = u32x2{rests_of(v[0], h[0]), rests_of(v[1], h[1])};
+            } else if (i < r.m && j < r.n) {
+              uint16_t* const out = reinterpret_cast<uint16_t*>(p.updates + r.update);
+              if (r.wide && r.cols % 8 == 0) {
+                const u32x2 lo = to_bf16(v[0]), hi = to_bf16(v[1]);
+                *reinterpret_cast<u32x4*>(out + uint64_t(i) * r.cols + j) = u32x4{lo.x, lo.y, hi.x, hi.y};
+              } else {
+#pragma unroll
+                for (uint32_t e = 0; e < 8; e++)
+                  if (j + e < r.n)
+                    out[r.wide ? uint64_t(i) * r.cols + j + e : uint64_t(j + e) * r.cols + i] =
+                        uint16_t(rne_bf16(as_u(v[e / 4][e % 4])));
+              }
+            }
+          }
+        }
+      };
+      if (p.last) finish(no, yes);
+      else if (p.carry) finish(yes, no);
+      else finish(no, no);
+    } else {
+      const f16* const A = reinterpret_cast<const f16*>(p.scratch + rec->a);
+      f16* const out = reinterpret_cast<f16*>(p.scratch + (kWhat == kGram ? rec->a : rec->q));
+      const uint32_t ld = rec->mp;
+      const float scale = kWhat == kGram ? kMuonLiftA / (rec->lift * rec->lift) : p.c * (1.0f / kMuonLiftA);
+      f16x8 x[M][N / 2];
+      if constexpr (kWhat == kPoly)
+#pragma unroll
+        for (uint32_t s = 0; s < M; s++)
+#pragma unroll
+          for (uint32_t c = 0; c < N / 2; c++)
+            x[s][c] = *reinterpret_cast<const f16x8*>(A + uint64_t(i1 + 16 * s) * ld + j1 + 32 * c);
+      // The mirror image goes by way of LDS, each wave's part by itself (whose LDS
+      // instructions are carried out in turn), 32 rows of WN at a time: chunks of 16
+      // bytes are permuted by their row, and a transposing read gives a lane four
+      // rows of its column.
+      constexpr uint32_t kChunks = T::WN / 8;
+      f16* const mirror = lds + Lds<T>::ring + wave * Lds<T>::mirror;
+#pragma unroll
+      for (uint32_t b = 0; b < M / 2; b++) {
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (uint32_t s = 2 * b; s < 2 * b + 2; s++)
+#pragma unroll
+          for (uint32_t c = 0; c < N / 2; c++) {
+            f16x8 h;
+#pragma unroll
+            for (uint32_t e = 0; e < 8; e++) {
+              const float v = scale * acc[s][2 * c + e / 4][e % 4];
+              h[e] = f16(kWhat == kPoly ? __builtin_fmaf(p.b, float(x[s][c][e]), v) : v);
+            }
+            *reinterpret_cast<f16x8*>(out + uint64_t(i1 + 16 * s) * ld + j1 + 32 * c) = h;
+            const uint32_t row = s % 2 * 16 + lane % 16, chunk = c * 4 + lane / 16;
+            *reinterpret_cast<f16x8*>(mirror + row * T::WN + (chunk ^ (row / 2 % kChunks)) * 8) = h;
+          }
+        if (diagonal) continue;
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (uint32_t q = 0; q < N; q++) {
+          const uint32_t row = lane / 16 * 8, column = q * 16 + lane % 4 * 4;
+          union {
+            f16x8 v;
+            i16x4 half[2];
+          } u;
+#pragma unroll
+          for (uint32_t h = 0; h < 2; h++) {
+            const uint32_t k = row + 4 * h + lane % 16 / 4;
+            u.half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (lds_i16x4*)(mirror + k * T::WN + ((column / 8) ^ (k / 2 % kChunks)) * 8 + column % 8));
+          }
+          *reinterpret_cast<f16x8*>(out + uint64_t(i2 + q * 16) * ld + j2 + 32 * b) = u.v;
+        }
+      }
+    }
+    if (!more) return;
   }
 }
 
 template <class T>
 int products(const MuonArgs& a, hipStream_t st) {
-  constexpr uint32_t lds = T::S * 2 * T::B * T::D * sizeof(f16);
   for (uint32_t s = 0; s < a.n_steps; s++) {
     ProductArgs p;
     p.recs = a.recs;
@@ -705,14 +756,16 @@ int products(const MuonArgs& a, hipStream_t st) {
     p.last = s + 1 == a.n_steps;
     p.carried = s == 0 || s + 2 < a.n_steps;
     p.carry = s + 3 < a.n_steps;
-    p.tiles = a.gram.d;
-    hipLaunchKernelGGL((k_muon_product<kGram, T>), dim3(uint32_t(a.gram.n)), dim3(T::threads), lds, st, p);
-    if (const int e = int(hipGetLastError())) return e;
-    hipLaunchKernelGGL((k_muon_product<kPoly, T>), dim3(uint32_t(a.gram.n)), dim3(T::threads), lds, st, p);
-    if (const int e = int(hipGetLastError())) return e;
-    p.tiles = a.whole.d;
-    hipLaunchKernelGGL((k_muon_product<kWhole, T>), dim3(uint32_t(a.whole.n)), dim3(T::threads), lds, st, p);
-    if (const int e = int(hipGetLastError())) return e;
+    const auto launch = [&](auto kernel, const MuonTiles& tiles) {
+      p.tiles = tiles.d;
+      p.n = uint32_t(tiles.n);
+      const uint32_t grid = T::B == kMuonLarge && p.n > a.units ? a.units : p.n;
+      hipLaunchKernelGGL(kernel, dim3(grid), dim3(T::threads), Lds<T>::bytes, st, p);
+      return int(hipGetLastError());
+    };
+    if (const int e = launch(k_muon_product<kGram, T>, a.gram)) return e;
+    if (const int e = launch(k_muon_product<kPoly, T>, a.gram)) return e;
+    if (const int e = launch(k_muon_product<kWhole, T>, a.whole)) return e;
   }
   return 0;
 }
