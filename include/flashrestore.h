@@ -834,7 +834,7 @@ typedef struct fr_embed_info {
 /* FR_E_INVAL: an entry outside the table, rows * cols other than its numel,
  * rows or cols 0, a wrong dtype; FR_E_ALIGN: a gradient offset not a multiple of
  * 16; FR_E_RANGE: a gradient past its arena, and where rows (or max_tokens / 32)
- * times the slices of 512 columns come to 2^26.
+ * times the slices of 512 columns come to 2^25.
  * Synchronous; outside graph capture. */
 int fr_embed_create(const fr_plan* plan, const fr_embed_desc* desc, uint64_t grad_arena_bytes, fr_embed** out);
 int fr_embed_get_info(const fr_embed* e, fr_embed_info* out);

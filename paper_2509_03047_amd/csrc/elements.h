@@ -1,5 +1,5 @@
-// Elements of tensors in 32 and 16 bits, four at a time, for the kernels that
-// walk over them.
+// Elements of tensors in 32 and 16 bits, four at a time, and sums over a wave,
+// for the kernels that walk over tensors.
 #pragma once
 
 #include "device.h"
@@ -70,6 +70,44 @@ __device__ __forceinline__ u32x2 to_bf16(const f32x4& x) {
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
   return u32x2{__builtin_bit_cast(uint32_t, __builtin_convertvector(x.xy, bf16x2)),
                __builtin_bit_cast(uint32_t, __builtin_convertvector(x.zw, bf16x2))};
+}
+
+// Sums over a wave of eight 64-bit values at once.  Each of the first steps
+// brings the lanes together in pairs that keep one half of the values each, so
+// that they take 4 + 2 + 1 exchanges and the last three steps are of one value:
+// 10 exchanges instead of 48.  Lane l ends with the total of value l / 8.
+template <int kCtrl>
+__device__ __forceinline__ u64 dpp64(u64 x) {
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0u, uint32_t(x), kCtrl, 0xF, 0xF, true);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0u, uint32_t(x >> 32), kCtrl, 0xF, 0xF, true);
+  return u64(hi) << 32 | lo;
+}
+// The sums of a with the lanes 32 (or 16) apart in the lanes whose bit 5 (4) is
+// clear, those of b in the others.
+template <int kLanes>
+__device__ __forceinline__ u64 halve(u64 a, u64 b) {
+  const uint32_t al = uint32_t(a), ah = uint32_t(a >> 32), bl = uint32_t(b), bh = uint32_t(b >> 32);
+  if constexpr (kLanes == 32) {
+    const auto lo = __builtin_amdgcn_permlane32_swap(al, bl, false, false);
+    const auto hi = __builtin_amdgcn_permlane32_swap(ah, bh, false, false);
+    return (u64(hi[0]) << 32 | lo[0]) + (u64(hi[1]) << 32 | lo[1]);
+  } else {
+    const auto lo = __builtin_amdgcn_permlane16_swap(al, bl, false, false);
+    const auto hi = __builtin_amdgcn_permlane16_swap(ah, bh, false, false);
+    return (u64(hi[0]) << 32 | lo[0]) + (u64(hi[1]) << 32 | lo[1]);
+  }
+}
+__device__ __forceinline__ u64 wave_totals(u64 (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; i++) x[i] = halve<32>(x[i], x[i + 4]);
+#pragma unroll
+  for (int i = 0; i < 2; i++) x[i] = halve<16>(x[i], x[i + 2]);
+  const bool upper = threadIdx.x & 8;
+  const u64 keep = upper ? x[1] : x[0], send = upper ? x[0] : x[1];
+  u64 t = keep + dpp64<0x128>(send);  // row_ror:8
+  t += dpp64<0x141>(t);               // row_half_mirror
+  t += dpp64<0x4E>(t);                // quad_perm: lanes 2 apart
+  return t + dpp64<0xB1>(t);          // and neighbours
 }
 
 }  // namespace

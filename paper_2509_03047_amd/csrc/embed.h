@@ -46,10 +46,10 @@ inline uint64_t embed_run_slots(uint64_t n) { return 2 * ((n + FR_EMBED_RUN - 1)
 // Whether the launches over so many rows, places or tokens have fewer than 2^32
 // threads.
 inline bool embed_waves_fit(uint64_t rows, uint32_t cols) {
-  return rows * ((cols + 64 * kEmbedVec - 1) / (64 * kEmbedVec)) < (uint64_t(1) << 26);
+  return rows * ((cols + 64 * kEmbedVec - 1) / (64 * kEmbedVec)) < (uint64_t(1) << 25);
 }
 inline bool embed_lanes_fit(uint64_t tokens, uint32_t cols) {
-  return tokens * ((cols + kEmbedVec - 1) / kEmbedVec) < (uint64_t(1) << 32) - 256;
+  return tokens * ((cols + 64 * kEmbedVec - 1) / (64 * kEmbedVec)) < (uint64_t(1) << 26) - 4;
 }
 
 int launch_embed_lookup(const EmbedArgs& a, void* stream);

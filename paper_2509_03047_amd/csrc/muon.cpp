@@ -121,7 +121,7 @@ int validate(const fr_tensor_desc* table, uint32_t n_entries, const Layout& L, u
   info.arena_bytes = arena_bytes;
   info.device = -1;
   bool twice = false, strange = false;
-  uint64_t tiles = 0;
+  uint64_t tiles = 0, subs = 0;
   for (uint32_t k = 0; k < n; k++) {
     const fr_muon_tensor& d = t[k];
     if (d.reserved || d.flags || d.group >= n_groups || !std::isfinite(d.scale)) return FR_E_INVAL;
@@ -177,13 +177,22 @@ int validate(const fr_tensor_desc* table, uint32_t n_entries, const Layout& L, u
     r.slot0 = tiles;
     r.slots = (numel + kMuonTile - 1) / kMuonTile;
     tiles += r.slots;
+    r.sub0 = subs;
+    subs += (numel + kMuonSub - 1) / kMuonSub;
   }
   lay_out_scratch(out);
   if (twice) return FR_E_OVERLAP;
   if (!disjoint(written) || !disjoint(updated)) return FR_E_OVERLAP;
   if (strange) return FR_E_INVAL;
-  // a launch has fewer than 2^32 threads
-  if (tiles >= (uint64_t(1) << 24) || info.n_elements >= (uint64_t(1) << 34)) return FR_E_RANGE;
+  // a launch has fewer than 2^32 threads, 256 or 512 a tile
+  uint64_t spread = 0, products = 0;
+  for (const MuonRec& r : out->recs) {
+    if (!r.numel) continue;
+    spread += uint64_t(r.mp) * r.np / 4096;
+    products += uint64_t(r.mp / out->side) * (r.np / out->side);
+  }
+  if (tiles >= (uint64_t(1) << 22) - 8 || spread >= (uint64_t(1) << 24) || products >= (uint64_t(1) << 23))
+    return FR_E_RANGE;
   return FR_OK;
 }
 
@@ -249,9 +258,12 @@ int build(fr_muon* o) {
   TileList gram, whole;
   std::vector<AdamwFold> mom, step;
   const bool sums = o->C >= FR_ADAMW_MIN_SUM_CHUNK;
-  uint64_t slots = 0;
-  for (const MuonRec& r : Y.recs) slots += r.slots;
-  const uint64_t stride = (slots + 7) / 8;
+  uint64_t slots = 0, subs = 0;
+  for (const MuonRec& r : Y.recs) {
+    slots += r.slots;
+    subs += (r.numel + kMuonSub - 1) / kMuonSub;
+  }
+  const uint64_t stride = (slots + 7) / 8, sub_stride = (subs + 7) / 8;
   walk.assign(8 * stride, 0);
   for (uint32_t k = 0; k < n; k++) {
     const MuonRec& r = Y.recs[k];
@@ -266,16 +278,15 @@ int build(fr_muon* o) {
       for (uint32_t j = 0; j <= i; j++) gram.items.push_back({id | uint64_t(i) << 16 | j, r.np});
     for (uint32_t j = 0; j < tn; j++)
       for (uint32_t i = 0; i < tm; i++) whole.items.push_back({id | uint64_t(i) << 16 | j, r.mp});
-    for (uint32_t i = 0; i < r.mp / 64; i++)
-      for (uint32_t j = 0; j < r.np / 64; j++) spread.push_back(id | uint64_t(i) << 16 | j);
+    for (uint64_t i = 0; i < uint64_t(r.mp) * r.np / 4096; i++) spread.push_back(id | i);
     if (!sums) continue;
     // chunk i of an array holds this many elements, and so these tiles
     const uint64_t per[3] = {o->C / 2, o->C / 4, o->C / 4};
     for (uint32_t j = 0; j < 3; j++)
       for (uint32_t i = 0; i < Y.n_chunks[size_t(k) * 3 + j]; i++) {
-        const uint64_t t = per[j] / kMuonTile;
-        const AdamwFold f = {Y.chunk0[size_t(k) * 3 + j] + i, uint32_t(r.slot0 + i * t),
-                             uint32_t(std::min(t, r.slots - i * t)), j == 2 ? 0 : j};
+        const uint64_t t = per[j] / kMuonSub, all = (r.numel + kMuonSub - 1) / kMuonSub;
+        const AdamwFold f = {Y.chunk0[size_t(k) * 3 + j] + i, uint32_t(r.sub0 + i * t),
+                             uint32_t(std::min(t, all - i * t)), j == 2 ? 0 : j};
         (j == 2 ? mom : step).push_back(f);
       }
   }
@@ -291,7 +302,7 @@ int build(fr_muon* o) {
   const size_t fs = c.add(step.data(), step.size() * sizeof(AdamwFold));
   const size_t np = c.add(nullptr, 8 * stride * sizeof(double));
   const size_t nf = c.add(nullptr, n * sizeof(double));
-  const size_t sp = c.add(nullptr, sums ? 2 * 8 * stride * sizeof(fr_chunk_sum) : 0);
+  const size_t sp = c.add(nullptr, sums ? 2 * 8 * sub_stride * sizeof(fr_chunk_sum) : 0);
   const size_t sc = c.add(nullptr, Y.scratch);
   o->layout.info.device_bytes = c.total;
   hipError_t e = hipMalloc(&o->mem, c.total);
@@ -322,6 +333,7 @@ int build(fr_muon* o) {
   a.side = Y.side;
   a.walk = AdamwWalk{reinterpret_cast<const uint64_t*>(at(wa)), slots, stride};
   a.scratch = at(sc);
+  a.sub_stride = sub_stride;
   a.parts = reinterpret_cast<double*>(at(np));
   a.factors = reinterpret_cast<double*>(at(nf));
   a.spread = MuonTiles{reinterpret_cast<const uint64_t*>(at(ts)), spread.size()};

@@ -20,16 +20,20 @@ struct alignas(16) MuonRec {
   uint64_t grad, update, param, master, mom;  // param: kNone if it has none
   uint64_t x[2], rest, a, q;
   uint64_t slot0, slots;  // its tiles in the walk over elements
+  uint64_t sub0;          // and its first sub-tile
   uint32_t cols, m, n, mp, np;
   uint32_t wide;      // rows <= cols: X has the matrix's own rows
   uint32_t grad_f32, group;
   float scale;
   float lift;         // the power of two that X is stored times
-  uint32_t pad_[4];
+  uint32_t pad_[2];
 };
 static_assert(sizeof(MuonRec) == 160, "MuonRec is 160 bytes");
 
-constexpr uint32_t kMuonTile = 1024;  // elements of a workgroup of the walk over elements
+// Elements of a workgroup of the walk over elements, and of those that make one
+// part of a chunk's sum.
+constexpr uint32_t kMuonTile = 4096, kMuonSub = 1024;
+static_assert(kMuonSub * 4 <= FR_ADAMW_MIN_SUM_CHUNK, "a sub-tile lies inside a chunk");
 // Sides of the products' tiles, to which those of matrices are padded.
 constexpr uint32_t kMuonLarge = 256, kMuonSmall = 64;
 constexpr float kMuonLiftA = 256.0f;  // A and Q are stored times this
@@ -56,13 +60,14 @@ struct MuonArgs {
   const void* grads = nullptr;
   void* updates = nullptr;
   bool momentum = false;   // of the state; else the gradients as they are
-  MuonTiles spread;  // tiles of 64 x 64
+  MuonTiles spread;  // (matrix << 32) | tile of 4,096 elements
   MuonTiles gram, whole;
   const fr_muon_coeffs* coeffs = nullptr;
   uint32_t n_steps = 0;
   // sums, or sum_parts == NULL
   uint64_t C = 0;
-  fr_chunk_sum* sum_parts = nullptr;
+  fr_chunk_sum* sum_parts = nullptr;  // by sub-tile, two arrays of 8 * sub_stride places
+  uint64_t sub_stride = 0;
   const AdamwFold* folds = nullptr;
   uint32_t n_folds = 0;
   fr_chunk_sum* sums = nullptr;

@@ -21,21 +21,28 @@ typedef f16 f16x8 __attribute__((ext_vector_type(8)));
 
 // ------------------------------------------------------- walks over elements
 
+// A workgroup takes kMuonTile elements, 4 kMuonSub: each thread four of each sub-tile,
+// all of whose loads are in flight together.  A sub-tile lies inside every array's
+// chunk.
+constexpr uint32_t kU = kMuonTile / kMuonSub;
+
 struct Elements {
   MuonRec r;
   uint64_t e0;     // the tile's first
   uint32_t n;      // how many it has
   uint32_t place;  // of the tile
+  uint64_t sub;    // its first sub-tile
 };
-__device__ __forceinline__ Elements elements_of(const AdamwWalk& w, const MuonRec* recs) {
+__device__ __forceinline__ Elements elements_of(const AdamwWalk& w, const MuonRec* recs, uint32_t block) {
   Elements t;
-  const uint64_t at = (blockIdx.x & 7) * w.stride + (blockIdx.x >> 3);
+  const uint64_t at = (block & 7) * w.stride + (block >> 3);
   const uint64_t slot = w.d[at];
   t.r = recs[slot >> 32];
-  t.e0 = uint64_t(uint32_t(slot)) * kMuonTile;
   const uint32_t j = uint32_t(slot), whole = uint32_t(t.r.numel / kMuonTile);
+  t.e0 = uint64_t(j) * kMuonTile;
   t.n = j < whole ? kMuonTile : uint32_t(t.r.numel) % kMuonTile;
   t.place = uint32_t(at);
+  t.sub = t.r.sub0 + uint64_t(j) * kU;
   return t;
 }
 
@@ -44,14 +51,41 @@ __device__ __forceinline__ f32x4 load_grad(const void* p, bool f32, uint32_t i, 
   return __builtin_bit_cast(f32x4, f32 ? load4<kFull>(p, i, n) : widen(load4h<kFull>(p, i, n)));
 }
 
-// The tile's sum of x (thread 0's) over its four waves.
-template <class T>
-__device__ __forceinline__ T tile_sum(T x) {
-  __shared__ T part[4];
+// The sum of x over the workgroup, in all threads.
+__device__ __forceinline__ double block_sum(double x) {
+  __shared__ double part[4];
   for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
   if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = x;
   __syncthreads();
   return part[0] + part[1] + part[2] + part[3];
+}
+
+// A tile's sums: s[u] and ws[u] of its sub-tiles, for `kinds` arrays in turn, added
+// up over the workgroup and left where the fold finds them.
+__device__ __forceinline__ void leave_sums(const MuonArgs& a, const Elements& t, uint32_t kind, const u64 (&s)[kU],
+                                           const u64 (&ws)[kU]) {
+  static_assert(kU == 4, "eight values");
+  u64 x[8];
+#pragma unroll
+  for (uint32_t u = 0; u < kU; u++) {
+    x[2 * u] = s[u];
+    x[2 * u + 1] = ws[u];
+  }
+  const u64 total = wave_totals(x);
+  __shared__ u64 part[2][4][8];
+  if (threadIdx.x % 8 == 0) part[kind][threadIdx.x / 64][threadIdx.x % 64 / 8] = total;
+  __syncthreads();
+  const uint32_t v = threadIdx.x, u = v / 2;
+  if (v < 8 && u * kMuonSub < t.n) {
+    const uint64_t g = t.sub + u, at = (g & 7) * a.sub_stride + (g >> 3);
+    reinterpret_cast<u64*>(a.sum_parts + uint64_t(kind) * 8 * a.sub_stride + at)[v % 2] =
+        part[kind][0][v] + part[kind][1][v] + part[kind][2][v] + part[kind][3][v];
+  }
+}
+
+// Word of sub-tile u's first element in its chunk, by bytes an element.
+__device__ __forceinline__ uint32_t word_of(const MuonArgs& a, const Elements& t, uint32_t u, uint32_t bytes) {
+  return uint32_t(bytes * (t.e0 + u * kMuonSub) & (a.C - 1)) / 4;
 }
 
 __device__ __forceinline__ float direction(float x, float m, float momentum, bool nesterov) {
@@ -62,97 +96,128 @@ __device__ __forceinline__ float direction(float x, float m, float momentum, boo
 // for, the momenta's words' sums.
 template <bool kMomentum, bool kSums, bool kFull>
 __device__ __forceinline__ void momentum_tile(const Elements& t, const MuonArgs& a) {
-  const uint32_t n = kFull ? kMuonTile : t.n, i = threadIdx.x * 4;
+  const uint32_t n = kFull ? kMuonTile : t.n;
   const uint8_t* const pg = static_cast<const uint8_t*>(a.grads) + t.r.grad + (t.r.grad_f32 ? 4 : 2) * t.e0;
-  f32x4 g = load_grad<kFull>(pg, t.r.grad_f32, i, n), d = g;
-  u64 s = 0, ws = 0;
-  if constexpr (kMomentum) {
-    uint8_t* const pm = static_cast<uint8_t*>(a.state) + t.r.mom + 4 * t.e0;
-    u32x4 um = load4<kFull>(pm, i, n);
-    const fr_muon_hyper h = a.hyper[t.r.group];
-    const fr_grad_stats st = *a.stats;
-    if (!st.nonfinite) {
-      f32x4 m = __builtin_bit_cast(f32x4, um);
+  uint8_t* const pm = static_cast<uint8_t*>(a.state) + t.r.mom + 4 * t.e0;
+  f32x4 g[kU];
+  u32x4 um[kU] = {};
 #pragma unroll
-      for (int j = 0; j < 4; j++) {
-        const float x = g[j] * st.scale;
-        m[j] = m[j] * h.momentum + x;
-        d[j] = direction(x, m[j], h.momentum, h.nesterov != 0);
-        if (!kFull && i + j >= n) m[j] = d[j] = 0.0f;  // (a scale may be NaN)
-      }
-      um = __builtin_bit_cast(u32x4, m);
-      store4<kFull>(pm, um, i, n);
-    }
-    if constexpr (kSums) acc4(um, uint32_t(4 * t.e0 & (a.C - 1)) / 4 + i, s, ws);
+  for (uint32_t u = 0; u < kU; u++) {
+    const uint32_t i = u * kMuonSub + threadIdx.x * 4;
+    if constexpr (kMomentum) um[u] = load4<kFull>(pm, i, n);
+    g[u] = load_grad<kFull>(pg, t.r.grad_f32, i, n);
+  }
+  fr_muon_hyper h = {};
+  fr_grad_stats st = {};
+  if constexpr (kMomentum) {
+    h = a.hyper[t.r.group];
+    st = *a.stats;
   }
   double q = 0;
+  u64 s[kU] = {}, ws[kU] = {};
 #pragma unroll
-  for (int j = 0; j < 4; j++) q += double(d[j]) * double(d[j]);
-  q = tile_sum(q);
-  if (threadIdx.x == 0) a.parts[t.place] = q;
-  if constexpr (kSums) {
-    s = tile_sum(s);
-    __syncthreads();
-    ws = tile_sum(ws);
-    if (threadIdx.x == 0) a.sum_parts[t.place] = fr_chunk_sum{s, ws};
+  for (uint32_t u = 0; u < kU; u++) {
+    const uint32_t i = u * kMuonSub + threadIdx.x * 4;
+    f32x4 d = g[u];
+    if constexpr (kMomentum) {
+      if (!st.nonfinite) {
+        f32x4 m = __builtin_bit_cast(f32x4, um[u]);
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+          const float x = g[u][j] * st.scale;
+          m[j] = m[j] * h.momentum + x;
+          d[j] = direction(x, m[j], h.momentum, h.nesterov != 0);
+          if (!kFull && i + j >= n) m[j] = d[j] = 0.0f;  // (a scale may be NaN)
+        }
+        um[u] = __builtin_bit_cast(u32x4, m);
+        store4<kFull>(pm, um[u], i, n);
+      }
+      if constexpr (kSums) acc4(um[u], word_of(a, t, u, 4) + threadIdx.x * 4, s[u], ws[u]);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; j++) q += double(d[j]) * double(d[j]);
   }
+  q = block_sum(q);
+  if (threadIdx.x == 0) a.parts[t.place] = q;
+  if constexpr (kSums) leave_sums(a, t, 0, s, ws);
 }
 
 template <bool kMomentum, bool kSums>
 __global__ __launch_bounds__(256) void k_muon_momentum(MuonArgs a) {
-  const Elements t = elements_of(a.walk, a.recs);
+  const Elements t = elements_of(a.walk, a.recs, blockIdx.x);
   if (t.n == kMuonTile) momentum_tile<kMomentum, kSums, true>(t, a);
   else momentum_tile<kMomentum, kSums, false>(t, a);
 }
 
-// One tile of the step.
-template <bool kSums, bool kFull>
+// One tile of the step, or with U = 1 (where nothing is summed) one sub-tile: an 8B
+// model's share takes 1.63 ms by sub-tiles and 1.78 by tiles, with sums 1.78 by tiles
+// and 2.1 by sub-tiles.
+template <uint32_t U, bool kFull>
 __device__ __forceinline__ void apply_tile(const Elements& t, const MuonArgs& a) {
-  const uint32_t n = kFull ? kMuonTile : t.n, i = threadIdx.x * 4;
+  constexpr bool kSums = U == kU;
+  const uint32_t n = kFull ? U * kMuonSub : t.n;
   uint8_t* const pw = static_cast<uint8_t*>(a.state) + t.r.master + 4 * t.e0;
   uint8_t* const pp = t.r.param == kNone ? nullptr : static_cast<uint8_t*>(a.state) + t.r.param + 2 * t.e0;
-  u32x4 uw = load4<kFull>(pw, i, n);
-  const f32x4 u = __builtin_bit_cast(
-      f32x4, widen(load4h<kFull>(static_cast<const uint8_t*>(a.updates) + t.r.update + 2 * t.e0, i, n)));
+  const uint8_t* const pu = static_cast<const uint8_t*>(a.updates) + t.r.update + 2 * t.e0;
+  u32x4 uw[U], uu[U];
+#pragma unroll
+  for (uint32_t k = 0; k < U; k++) {
+    const uint32_t i = k * kMuonSub + threadIdx.x * 4;
+    uw[k] = load4<kFull>(pw, i, n);
+    uu[k] = load4h<kFull>(pu, i, n);
+  }
   const fr_muon_hyper h = a.hyper[t.r.group];
   const bool skip = a.stats->nonfinite != 0;
-  u32x2 up = {0, 0};
-  if (!skip) {
-    const float keep = 1.0f - h.lr * h.weight_decay, step = h.lr * t.r.scale;
-    f32x4 w = __builtin_bit_cast(f32x4, uw);
+  const float keep = 1.0f - h.lr * h.weight_decay, step = h.lr * t.r.scale;
+  u64 s[2][U] = {}, ws[2][U] = {};
 #pragma unroll
-    for (int j = 0; j < 4; j++) {
-      w[j] = w[j] * keep - u[j] * step;
-      if (!kFull && i + j >= n) w[j] = 0.0f;
+  for (uint32_t k = 0; k < U; k++) {
+    const uint32_t i = k * kMuonSub + threadIdx.x * 4;
+    u32x2 up = {0, 0};
+    if (!skip) {
+      f32x4 w = __builtin_bit_cast(f32x4, uw[k]);
+      const f32x4 u = __builtin_bit_cast(f32x4, widen(uu[k]));
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        w[j] = w[j] * keep - u[j] * step;
+        if (!kFull && i + j >= n) w[j] = 0.0f;
+      }
+      uw[k] = __builtin_bit_cast(u32x4, w);
+      up = to_bf16(w);
+      store4<kFull>(pw, uw[k], i, n);
+      if (pp) store4h<kFull>(pp, up, i, n);
+    } else if (kSums && pp) {
+      const u32x4 x = widen(load4h<kFull>(pp, i, n));
+      up = u32x2{x.x >> 16 | x.y, x.z >> 16 | x.w};
     }
-    uw = __builtin_bit_cast(u32x4, w);
-    up = to_bf16(w);
-    store4<kFull>(pw, uw, i, n);
-    if (pp) store4h<kFull>(pp, up, i, n);
-  } else if (kSums && pp) {
-    const u32x4 x = widen(load4h<kFull>(pp, i, n));
-    up = u32x2{x.x >> 16 | x.y, x.z >> 16 | x.w};
+    if constexpr (kSums) {
+      acc2(up, word_of(a, t, k, 2) + threadIdx.x * 2, s[0][k], ws[0][k]);
+      acc4(uw[k], word_of(a, t, k, 4) + threadIdx.x * 4, s[1][k], ws[1][k]);
+    }
   }
   if constexpr (kSums) {
-    u64 s[2] = {}, ws[2] = {};
-    acc2(up, uint32_t(2 * t.e0 & (a.C - 1)) / 4 + i / 2, s[0], ws[0]);
-    acc4(uw, uint32_t(4 * t.e0 & (a.C - 1)) / 4 + i, s[1], ws[1]);
-#pragma unroll
-    for (int k = 0; k < 2; k++) {
-      s[k] = tile_sum(s[k]);
-      __syncthreads();
-      ws[k] = tile_sum(ws[k]);
-      __syncthreads();
-      if (threadIdx.x == 0) a.sum_parts[uint64_t(k) * 8 * a.walk.stride + t.place] = fr_chunk_sum{s[k], ws[k]};
-    }
+    leave_sums(a, t, 0, s[0], ws[0]);
+    leave_sums(a, t, 1, s[1], ws[1]);
   }
 }
 
 template <bool kSums>
 __global__ __launch_bounds__(256) void k_muon_apply(MuonArgs a) {
-  const Elements t = elements_of(a.walk, a.recs);
-  if (t.n == kMuonTile) apply_tile<kSums, true>(t, a);
-  else apply_tile<kSums, false>(t, a);
+  if constexpr (kSums) {
+    const Elements t = elements_of(a.walk, a.recs, blockIdx.x);
+    if (t.n == kMuonTile) apply_tile<kU, true>(t, a);
+    else apply_tile<kU, false>(t, a);
+  } else {
+    // sub-tile u of a tile, on the die that the tile belongs to
+    const uint32_t u = blockIdx.x / 8 % kU, b = blockIdx.x / (8 * kU) * 8 + blockIdx.x % 8;
+    if (b >= a.walk.n) return;
+    Elements t = elements_of(a.walk, a.recs, b);
+    if (u * kMuonSub >= t.n) return;
+    t.e0 += u * kMuonSub;
+    t.n = t.n - u * kMuonSub < kMuonSub ? t.n - u * kMuonSub : kMuonSub;
+    if (t.n == kMuonSub) apply_tile<1, true>(t, a);
+    else apply_tile<1, false>(t, a);
+  }
 }
 
 // A matrix's norm, and what its elements are multiplied by to be X_0 as it is
@@ -164,7 +229,7 @@ __global__ __launch_bounds__(256) void k_muon_norm(MuonArgs a) {
     const uint64_t g = r.slot0 + i;
     q += a.parts[(g & 7) * a.walk.stride + (g >> 3)];
   }
-  q = tile_sum(q);
+  q = block_sum(q);
   if (threadIdx.x == 0) {
     const double f = double(r.lift) / (__builtin_sqrt(q) + double(a.hyper[r.group].eps));
     a.factors[blockIdx.x] = q == 0.0 ? 0.0 : __builtin_isfinite(q) ? f : __builtin_nan("");
@@ -224,10 +289,9 @@ __device__ __forceinline__ f32x4 load_four(const void* p, uint64_t at, uint32_t 
   return v;
 }
 
-// X_0 of a tile of 64 x 64 elements; zeros behind the matrix's sides.  The
-// matrix is read along its own rows; if those are X's columns, by way of LDS.
-constexpr uint32_t kSpread = 64;
-
+// X_0 of a tile of 4,096 elements; zeros behind the matrix's sides.  The matrix is
+// read along its own rows: 16 of 256 elements where they are X's and there are
+// so many, else 64 of 64, by way of LDS where they are X's columns.
 template <bool kGrad32>
 __device__ __forceinline__ f32x4 spread_four(const MuonArgs& a, const MuonRec& r, const fr_muon_hyper& h, float scale,
                                              double f, uint32_t row, uint32_t col, uint32_t rows) {
@@ -249,24 +313,26 @@ __device__ __forceinline__ f32x4 spread_four(const MuonArgs& a, const MuonRec& r
 __global__ __launch_bounds__(256) void k_muon_spread(MuonArgs a) {
   if (a.stats->nonfinite) return;
   const uint64_t tile = a.spread.d[blockIdx.x];
-  const uint32_t id = uint32_t(tile >> 32), i0 = uint32_t(tile >> 16 & 0xFFFF) * kSpread,
-                 j0 = uint32_t(tile & 0xFFFF) * kSpread;
+  const uint32_t id = uint32_t(tile >> 32);
   const MuonRec r = a.recs[id];
+  const bool flat = r.wide && r.np % 256 == 0;
+  const uint32_t side = flat ? 256 : 64, across = r.np / side;
+  const uint32_t i0 = uint32_t(tile) / across * (4096 / side), j0 = uint32_t(tile) % across * side;
   const double f = a.factors[id];
   const fr_muon_hyper h = a.hyper[r.group];
   const float scale = a.stats->scale;
   f16* const x = reinterpret_cast<f16*>(a.scratch + r.x[0]);
   uint8_t* const rest = a.scratch + r.rest;
-  const uint32_t lo = threadIdx.x % 16 * 4, hi = threadIdx.x / 16;
+  const uint32_t lo = threadIdx.x % (side / 4) * 4, hi = threadIdx.x / (side / 4), down = 1024 / side;
   f32x4 v[4];
 #pragma unroll
   for (uint32_t k = 0; k < 4; k++) {
-    const uint32_t row = (r.wide ? i0 : j0) + hi + 16 * k, col = (r.wide ? j0 : i0) + lo;
+    const uint32_t row = (r.wide ? i0 : j0) + hi + down * k, col = (r.wide ? j0 : i0) + lo;
     v[k] = r.grad_f32 ? spread_four<true>(a, r, h, scale, f, row, col, r.wide ? r.m : r.n)
                       : spread_four<false>(a, r, h, scale, f, row, col, r.wide ? r.m : r.n);
   }
   if (!r.wide) {
-    __shared__ float t[kSpread][kSpread + 1];
+    __shared__ float t[64][64 + 1];
 #pragma unroll
     for (uint32_t k = 0; k < 4; k++)
 #pragma unroll
@@ -279,7 +345,7 @@ __global__ __launch_bounds__(256) void k_muon_spread(MuonArgs a) {
   }
 #pragma unroll
   for (uint32_t k = 0; k < 4; k++) {
-    const uint64_t at = uint64_t(i0 + hi + 16 * k) * r.np + j0 + lo;
+    const uint64_t at = uint64_t(i0 + hi + down * k) * r.np + j0 + lo;
     const f16x4 y = __builtin_convertvector(v[k], f16x4);
     *reinterpret_cast<f16x4*>(x + at) = y;
     *reinterpret_cast<uint32_t*>(rest + at) = rests_of(v[k], y);
@@ -773,13 +839,13 @@ int products(const MuonArgs& a, hipStream_t st) {
 int fold(const MuonArgs& a, hipStream_t st) {
   if (!a.sum_parts || !a.n_folds) return 0;
   AdamwStepArgs f;
-  f.walk = a.walk;
+  f.walk.stride = a.sub_stride;
   f.folds = a.folds;
   f.n_folds = a.n_folds;
   f.parts = a.sum_parts;
   f.state = a.state;
   f.sums = a.sums;
-  return launch_adamw_fold(f, a.C / 2 / kMuonTile, st);
+  return launch_adamw_fold(f, a.C / 2 / kMuonSub, st);
 }
 
 }  // namespace
@@ -803,9 +869,9 @@ int launch_muon_direction(const MuonArgs& a, void* stream) {
 int launch_muon_apply(const MuonArgs& a, void* stream) {
   const hipStream_t st = hipStream_t(stream);
   if (a.walk.n == 0) return 0;
-  const dim3 tiles(uint32_t(a.walk.n));
-  if (a.sum_parts) hipLaunchKernelGGL(k_muon_apply<true>, tiles, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(k_muon_apply<false>, tiles, dim3(256), 0, st, a);
+  const uint32_t tiles = uint32_t(a.walk.n);
+  if (a.sum_parts) hipLaunchKernelGGL(k_muon_apply<true>, dim3(tiles), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(k_muon_apply<false>, dim3((tiles + 7) / 8 * 8 * kU), dim3(256), 0, st, a);
   if (const int e = int(hipGetLastError())) return e;
   return fold(a, st);
 }
