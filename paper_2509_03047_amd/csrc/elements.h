@@ -64,6 +64,13 @@ __device__ __forceinline__ void store4h(void* p, u32x2 x, uint32_t i, uint32_t n
     if (i + j < n) q[j] = uint16_t(x[j / 2] >> (16 * (j & 1)));
 }
 
+// Vectors at any element's address: the memory system takes accesses that are not
+// aligned, and the compiler makes one of each (which it does not of a structure of
+// elements).
+typedef uint32_t u32x4_at2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x2_at2 __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
+
 // Four fp32 patterns to bf16, two a word: v_cvt_pk_bf16_f32 rounds every
 // pattern as rne_bf16 does, NaNs included.
 __device__ __forceinline__ u32x2 to_bf16(const f32x4& x) {

@@ -17,7 +17,8 @@ struct fr_embed {
   uint64_t offset = 0;       // of the table in the state
   uint64_t grad_offset = 0;
   void* mem = nullptr;       // the scratch below
-  uint32_t *order = nullptr, *row_of = nullptr, *start = nullptr;
+  uint32_t *order = nullptr, *row_of = nullptr;
+  Places* places = nullptr;
   float* runs = nullptr;
 };
 
@@ -58,9 +59,9 @@ int build(fr_embed* e) {
   const uint64_t T = e->info.max_tokens;
   if (!T) return FR_OK;
   const auto up = [](uint64_t x) { return (x + 255) & ~uint64_t(255); };
-  const uint64_t order = up(T * 4), start = up((e->info.rows + 1) * 4);
+  const uint64_t order = up(T * 4), places = up((e->info.rows + 1) * sizeof(Places));
   const uint64_t runs = up(embed_run_slots(T) * e->info.cols * 4);
-  const uint64_t total = 2 * order + start + runs;
+  const uint64_t total = 2 * order + places + runs;
   const hipError_t rc = hipMalloc(&e->mem, total);
   if (rc != hipSuccess) {
     e->mem = nullptr;
@@ -70,8 +71,8 @@ int build(fr_embed* e) {
   uint8_t* p = static_cast<uint8_t*>(e->mem);
   e->order = reinterpret_cast<uint32_t*>(p);
   e->row_of = reinterpret_cast<uint32_t*>(p + order);
-  e->start = reinterpret_cast<uint32_t*>(p + 2 * order);
-  e->runs = reinterpret_cast<float*>(p + 2 * order + start);
+  e->places = reinterpret_cast<Places*>(p + 2 * order);
+  e->runs = reinterpret_cast<float*>(p + 2 * order + places);
   e->info.device_bytes = total;
   return FR_OK;
 }
@@ -194,7 +195,7 @@ extern "C" int fr_embed_grad(const fr_embed* e, const void* ids, uint32_t id_byt
   a.add = add != 0;
   a.order = e->order;
   a.row_of = e->row_of;
-  a.start = e->start;
+  a.places = e->places;
   a.runs = e->runs;
   return launch_result(launch_embed_grad(a, stream));
 }

@@ -10,7 +10,12 @@ namespace fr {
 // The workgroups that order the tokens have 16 waves, and each up to
 // kEmbedRows rows, whose counts by wave it keeps in LDS.
 constexpr uint32_t kEmbedVec = 8;  // columns of a lane
-constexpr uint32_t kEmbedWaves = 16, kEmbedRows = 512, kEmbedGroups = 256;
+constexpr uint32_t kEmbedWaves = 16, kEmbedRows = 512, kEmbedGroupsLog = 8;
+
+// A row's tokens, by their places in the order.
+struct Places {
+  uint32_t first, n;
+};
 
 struct EmbedArgs {
   uint64_t first = 0;
@@ -31,15 +36,10 @@ struct EmbedArgs {
   bool grad_f32 = false, add = false;
   uint32_t* order = nullptr;   // tokens by row, ascending
   uint32_t* row_of = nullptr;  // the row of each of these places
-  uint32_t* start = nullptr;   // each row's first place; rows + 1
-  float* runs = nullptr;       // sums of runs, by embed_run_slot
+  Places* places = nullptr;    // of each row; behind them how many all have
+  float* runs = nullptr;       // sums of runs of long rows
 };
 
-// Rows that a workgroup of the ordering has.
-inline uint32_t embed_group_rows(uint32_t rows) {
-  const uint32_t r = (rows + kEmbedGroups - 1) / kEmbedGroups;
-  return r < kEmbedRows ? r : kEmbedRows;
-}
 // Places of the sums of runs that n tokens can have.
 inline uint64_t embed_run_slots(uint64_t n) { return 2 * ((n + FR_EMBED_RUN - 1) / FR_EMBED_RUN) + 2; }
 

@@ -259,25 +259,16 @@ __device__ __forceinline__ uint32_t rests_of(const f32x4& v, const f16x4& h) {
   return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], w, true));
 }
 
-// Four elements of a row of n from any element's address on, zeros behind them.
-struct __attribute__((packed, aligned(2))) Half4 {
-  uint16_t x[4];
-};
-struct __attribute__((packed, aligned(4))) Float4 {
-  float x[4];
-};
+// Four elements from any element's address on, zeros behind the `left` that there are.
 template <bool kF32>
 __device__ __forceinline__ f32x4 load_four(const void* p, uint64_t at, uint32_t left) {
   f32x4 v = {0, 0, 0, 0};
   if (left >= 4) {
     if constexpr (kF32) {
-      const Float4 f = *reinterpret_cast<const Float4*>(static_cast<const float*>(p) + at);
-#pragma unroll
-      for (int j = 0; j < 4; j++) v[j] = f.x[j];
+      v = __builtin_bit_cast(f32x4, u32x4(*reinterpret_cast<const u32x4_at4*>(static_cast<const float*>(p) + at)));
     } else {
-      const Half4 h = *reinterpret_cast<const Half4*>(static_cast<const uint16_t*>(p) + at);
-#pragma unroll
-      for (int j = 0; j < 4; j++) v[j] = as_f(uint32_t(h.x[j]) << 16);
+      const u32x2 h = *reinterpret_cast<const u32x2_at2*>(static_cast<const uint16_t*>(p) + at);
+      v = __builtin_bit_cast(f32x4, u32x4{h.x << 16, h.x & 0xFFFF0000u, h.y << 16, h.y & 0xFFFF0000u});
     }
     return v;
   }
