@@ -94,7 +94,8 @@ void lay_out_scratch(MuonLayout* out) {
     const struct {
       uint64_t* where;
       uint64_t bytes;
-    } parts[5] = {{&r.x[0], 2 * wide}, {&r.x[1], 2 * wide}, {&r.rest, wide}, {&r.a, 2 * square}, {&r.q, 2 * square}};
+    } parts[7] = {{&r.x[0], 2 * wide}, {&r.x[1], 2 * wide}, {&r.rest, wide},     {&r.a, 2 * square},
+                  {&r.q, 2 * square},  {&r.da, 4ull * r.mp},  {&r.dq, 4ull * r.mp}};
     for (const auto& p : parts) {
       *p.where = out->scratch;
       out->scratch += p.bytes;

@@ -14,11 +14,12 @@ namespace fr {
 // and, for what the products read and write, the optimizer's scratch:
 //   x     mp x np, fp16    X, twice: read and written in turn
 //   rest  mp x np, 8 bits  what X is more than its fp16 number (e4m3)
-//   a, q  mp x mp, fp16    X X^T and the polynomial of it
+//   a, q  mp x mp, fp16    X X^T and the polynomial of it, with
+//   da, dq  mp, fp32       what their diagonals are more
 struct alignas(16) MuonRec {
   uint64_t numel;
   uint64_t grad, update, param, master, mom;  // param: kNone if it has none
-  uint64_t x[2], rest, a, q;
+  uint64_t x[2], rest, a, q, da, dq;
   uint64_t slot0, slots;  // its tiles in the walk over elements
   uint64_t sub0;          // and its first sub-tile
   uint32_t cols, m, n, mp, np;
@@ -28,7 +29,7 @@ struct alignas(16) MuonRec {
   float lift;         // the power of two that X is stored times
   uint32_t pad_[2];
 };
-static_assert(sizeof(MuonRec) == 160, "MuonRec is 160 bytes");
+static_assert(sizeof(MuonRec) == 176, "MuonRec is 176 bytes");
 
 // Elements of a workgroup of the walk over elements, and of those that make one
 // part of a chunk's sum.

@@ -554,6 +554,39 @@ struct Place {
   }
 };
 
+// A wave's way to the other side of the diagonal: 32 rows of its WN columns in 16
+// bits, written as they lie and read by columns.  Chunks of 16 bytes are permuted
+// by their row; a transposing read gives a lane four rows of its column.  (A
+// wave's LDS instructions are carried out in turn.)
+template <class T>
+struct Mirror {
+  static constexpr uint32_t kChunks = T::WN / 8;
+  f16* at;
+  __device__ __forceinline__ Mirror(f16* lds, uint32_t wave) : at(lds + Lds<T>::ring + wave * Lds<T>::mirror) {}
+  // row lane % 16 of the first or second 16, columns 32 c + 8 (lane / 16) ... + 7
+  template <class V>
+  __device__ __forceinline__ void write(uint32_t half, uint32_t c, const V& v) const {
+    static_assert(sizeof(V) == 16, "eight of 16 bits");
+    const uint32_t lane = threadIdx.x % 64, row = half * 16 + lane % 16, chunk = c * 4 + lane / 16;
+    *reinterpret_cast<V*>(at + row * T::WN + (chunk ^ (row / 2 % kChunks)) * 8) = v;
+  }
+  // rows 8 (lane / 16) ... + 7 of column 16 q + lane % 16
+  __device__ __forceinline__ u32x4 read(uint32_t q) const {
+    const uint32_t lane = threadIdx.x % 64, column = q * 16 + lane % 4 * 4;
+    union {
+      u32x4 v;
+      i16x4 half[2];
+    } u;
+#pragma unroll
+    for (uint32_t h = 0; h < 2; h++) {
+      const uint32_t k = lane / 16 * 8 + 4 * h + lane % 16 / 4;
+      u.half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (lds_i16x4*)(at + k * T::WN + ((column / 8) ^ (k / 2 % kChunks)) * 8 + column % 8));
+    }
+    return u.v;
+  }
+};
+
 // Tiles of L R (kWhole, with R's columns along the sum) or L R^T, one after
 // another: the next one's first slices are loaded while one's results are stored.
 template <MuonProduct kWhat, class T>
@@ -564,6 +597,7 @@ __global__ __launch_bounds__(T::threads) void k_muon_product(ProductArgs p) {
   constexpr uint32_t kLoads = 2 * kSlice / (8 * T::threads);  // of a wave, a slice of both operands
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
   const uint32_t wi = wave / (T::B / T::WN) * T::WM, wj = wave % (T::B / T::WN) * T::WN;
+  const Mirror<T> mirror(lds, wave);
   typedef Place<kWhat, T> Here;
   Here here = Here::of(p, blockIdx.x, wave);
   f32x4 acc[M][N];
@@ -638,7 +672,11 @@ __global__ __launch_bounds__(T::threads) void k_muon_product(ProductArgs p) {
     // times kMuonLiftA.
     if constexpr (kWhat == kWhole) {
       const f16* const X = reinterpret_cast<const f16*>(p.scratch + here.rec->x[p.flip]);
-      const float a = p.a * kMuonLiftA, b = a / kRestLift;
+      // (Q's part that its fp16 diagonal leaves out goes with a)
+      const float* const dq = reinterpret_cast<const float*>(p.scratch + here.rec->dq) + i1;
+      float a[M];
+#pragma unroll
+      for (uint32_t s = 0; s < M; s++) a[s] = p.a * kMuonLiftA + dq[16 * s];
       f16x8 x[M][N / 2];
 #pragma unroll
       for (uint32_t s = 0; s < M; s++)
@@ -660,7 +698,8 @@ __global__ __launch_bounds__(T::threads) void k_muon_product(ProductArgs p) {
             const f32x4 more = rests(z[s][q / 2][q % 2]);
 #pragma unroll
             for (uint32_t e = 0; e < 4; e++)
-              acc[s][q][e] = __builtin_fmaf(float(x[s][q / 2][q % 2 * 4 + e]), a, more[e] * b);
+              acc[s][q][e] =
+                  __builtin_fmaf(float(x[s][q / 2][q % 2 * 4 + e]), a[s], more[e] * (a[s] * (1.0f / kRestLift)));
           }
       } else {
 #pragma unroll
@@ -668,7 +707,7 @@ __global__ __launch_bounds__(T::threads) void k_muon_product(ProductArgs p) {
 #pragma unroll
           for (uint32_t q = 0; q < N; q++)
 #pragma unroll
-            for (uint32_t e = 0; e < 4; e++) acc[s][q][e] = a * float(x[s][q / 2][q % 2 * 4 + e]);
+            for (uint32_t e = 0; e < 4; e++) acc[s][q][e] = a[s] * float(x[s][q / 2][q % 2 * 4 + e]);
       }
     } else {
 #pragma unroll
@@ -707,6 +746,36 @@ __global__ __launch_bounds__(T::threads) void k_muon_product(ProductArgs p) {
       f16* const to = reinterpret_cast<f16*>(p.scratch + r.x[p.flip ^ 1]);
       uint8_t* const rest = p.scratch + r.rest;
       const float down = (p.last ? 1.0f / r.lift : 1.0f) / kMuonLiftA;
+      // (of a matrix that is tall its rows are X's columns)
+      const auto finish_tall = [&] {
+        uint16_t* const out = reinterpret_cast<uint16_t*>(p.updates + r.update);
+#pragma unroll
+        for (uint32_t b = 0; b < M / 2; b++) {
+          asm volatile("" ::: "memory");
+#pragma unroll
+          for (uint32_t s = 2 * b; s < 2 * b + 2; s++)
+#pragma unroll
+            for (uint32_t c = 0; c < N / 2; c++) {
+              const u32x2 lo = to_bf16(acc[s][2 * c] * down), hi = to_bf16(acc[s][2 * c + 1] * down);
+              mirror.write(s % 2, c, u32x4{lo.x, lo.y, hi.x, hi.y});
+            }
+          asm volatile("" ::: "memory");
+#pragma unroll
+          for (uint32_t q = 0; q < N; q++) {
+            const u32x4 v = mirror.read(q);
+            const uint32_t row = i2 + q * 16, col = j2 + 32 * b;  // of the matrix
+            if (row >= r.n || col >= r.m) continue;
+            uint16_t* const to_row = out + uint64_t(row) * r.cols + col;
+            if (col + 8 <= r.m) {
+              *reinterpret_cast<u32x4_at2*>(to_row) = v;
+            } else {
+#pragma unroll
+              for (uint32_t e = 0; e < 8; e++)
+                if (col + e < r.m) to_row[e] = uint16_t(v[e / 2] >> (16 * (e % 2)));
+            }
+          }
+        }
+      };
       const auto finish = [&](auto carry, auto last) {
 #pragma unroll
         for (uint32_t s = 0; s < M; s++) {
@@ -723,75 +792,81 @@ __global__ __launch_bounds__(T::threads) void k_muon_product(ProductArgs p) {
                 *reinterpret_cast<u32x2*>(rest + to_at) = u32x2{rests_of(v[0], h[0]), rests_of(v[1], h[1])};
             } else if (i < r.m && j < r.n) {
               uint16_t* const out = reinterpret_cast<uint16_t*>(p.updates + r.update);
-              if (r.wide && r.cols % 8 == 0) {
-                const u32x2 lo = to_bf16(v[0]), hi = to_bf16(v[1]);
-                *reinterpret_cast<u32x4*>(out + uint64_t(i) * r.cols + j) = u32x4{lo.x, lo.y, hi.x, hi.y};
+              uint16_t* const to_row = out + uint64_t(i) * r.cols + j;
+              const u32x2 lo = to_bf16(v[0]), hi = to_bf16(v[1]);
+              const u32x4 w = {lo.x, lo.y, hi.x, hi.y};
+              if (j + 8 <= r.n) {
+                *reinterpret_cast<u32x4_at2*>(to_row) = w;
               } else {
 #pragma unroll
                 for (uint32_t e = 0; e < 8; e++)
-                  if (j + e < r.n)
-                    out[r.wide ? uint64_t(i) * r.cols + j + e : uint64_t(j + e) * r.cols + i] =
-                        uint16_t(rne_bf16(as_u(v[e / 4][e % 4])));
+                  if (j + e < r.n) to_row[e] = uint16_t(w[e / 2] >> (16 * (e % 2)));
               }
             }
           }
         }
       };
-      if (p.last) finish(no, yes);
+      if (p.last && !r.wide) finish_tall();
+      else if (p.last) finish(no, yes);
       else if (p.carry) finish(yes, no);
       else finish(no, no);
     } else {
+      // The rounding of a diagonal, unlike that of other elements, does not average
+      // out: what it leaves is kept, and counts in what follows.  With e = A's,
+      //   Q = b A + c A A = b (A + diag(e)) + c (A A + diag(e) A + A diag(e))
+      // of the fp16 A (but for e^2).
       const f16* const A = reinterpret_cast<const f16*>(p.scratch + rec->a);
+      const float* const da = reinterpret_cast<const float*>(p.scratch + rec->da);
       f16* const out = reinterpret_cast<f16*>(p.scratch + (kWhat == kGram ? rec->a : rec->q));
+      float* const left = reinterpret_cast<float*>(p.scratch + (kWhat == kGram ? rec->da : rec->dq));
       const uint32_t ld = rec->mp;
       const float scale = kWhat == kGram ? kMuonLiftA / (rec->lift * rec->lift) : p.c * (1.0f / kMuonLiftA);
-      f16x8 x[M][N / 2];
+      f32x4 ej[N / 2][2];
       if constexpr (kWhat == kPoly)
 #pragma unroll
-        for (uint32_t s = 0; s < M; s++)
+        for (uint32_t c = 0; c < N / 2; c++)
 #pragma unroll
-          for (uint32_t c = 0; c < N / 2; c++)
-            x[s][c] = *reinterpret_cast<const f16x8*>(A + uint64_t(i1 + 16 * s) * ld + j1 + 32 * c);
-      // The mirror image goes by way of LDS, each wave's part by itself (whose LDS
-      // instructions are carried out in turn), 32 rows of WN at a time: chunks of 16
-      // bytes are permuted by their row, and a transposing read gives a lane four
-      // rows of its column.
-      constexpr uint32_t kChunks = T::WN / 8;
-      f16* const mirror = lds + Lds<T>::ring + wave * Lds<T>::mirror;
+          for (uint32_t k = 0; k < 2; k++) ej[c][k] = *reinterpret_cast<const f32x4*>(da + j1 + 32 * c + 4 * k);
 #pragma unroll
       for (uint32_t b = 0; b < M / 2; b++) {
         asm volatile("" ::: "memory");
+        f16x8 x[2][N / 2];
+        float ei[2];
+        if constexpr (kWhat == kPoly)
+#pragma unroll
+          for (uint32_t s = 0; s < 2; s++) {
+            const uint32_t i = i1 + 16 * (2 * b + s);
+            ei[s] = da[i];
+#pragma unroll
+            for (uint32_t c = 0; c < N / 2; c++)
+              x[s][c] = *reinterpret_cast<const f16x8*>(A + uint64_t(i) * ld + j1 + 32 * c);
+          }
 #pragma unroll
         for (uint32_t s = 2 * b; s < 2 * b + 2; s++)
 #pragma unroll
           for (uint32_t c = 0; c < N / 2; c++) {
+            const uint32_t i = i1 + 16 * s, j = j1 + 32 * c;
             f16x8 h;
 #pragma unroll
             for (uint32_t e = 0; e < 8; e++) {
-              const float v = scale * acc[s][2 * c + e / 4][e % 4];
-              h[e] = f16(kWhat == kPoly ? __builtin_fmaf(p.b, float(x[s][c][e]), v) : v);
+              float v = scale * acc[s][2 * c + e / 4][e % 4];
+              const bool on = diagonal && i == j + e;
+              if constexpr (kWhat == kPoly) {
+                const float was = float(x[s % 2][c][e]), ee = ei[s % 2] + ej[c][e / 4][e % 4];
+                v = __builtin_fmaf(__builtin_fmaf(scale, ee, p.b), was, v);
+                if (on) v = __builtin_fmaf(p.b, ei[s % 2], v);
+              }
+              h[e] = f16(v);
+              if (on) left[i] = v - float(h[e]);
             }
-            *reinterpret_cast<f16x8*>(out + uint64_t(i1 + 16 * s) * ld + j1 + 32 * c) = h;
-            const uint32_t row = s % 2 * 16 + lane % 16, chunk = c * 4 + lane / 16;
-            *reinterpret_cast<f16x8*>(mirror + row * T::WN + (chunk ^ (row / 2 % kChunks)) * 8) = h;
+            *reinterpret_cast<f16x8*>(out + uint64_t(i) * ld + j) = h;
+            mirror.write(s % 2, c, h);
           }
         if (diagonal) continue;
         asm volatile("" ::: "memory");
 #pragma unroll
-        for (uint32_t q = 0; q < N; q++) {
-          const uint32_t row = lane / 16 * 8, column = q * 16 + lane % 4 * 4;
-          union {
-            f16x8 v;
-            i16x4 half[2];
-          } u;
-#pragma unroll
-          for (uint32_t h = 0; h < 2; h++) {
-            const uint32_t k = row + 4 * h + lane % 16 / 4;
-            u.half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (lds_i16x4*)(mirror + k * T::WN + ((column / 8) ^ (k / 2 % kChunks)) * 8 + column % 8));
-          }
-          *reinterpret_cast<f16x8*>(out + uint64_t(i2 + q * 16) * ld + j2 + 32 * b) = u.v;
-        }
+        for (uint32_t q = 0; q < N; q++)
+          *reinterpret_cast<u32x4*>(out + uint64_t(i2 + q * 16) * ld + j2 + 32 * b) = mirror.read(q);
       }
     }
     if (!more) return;
