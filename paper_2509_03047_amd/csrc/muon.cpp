@@ -39,6 +39,7 @@ struct MuonLayout {
   // first chunks, and how many, of each matrix's param, master and momentum
   std::vector<uint32_t> chunk0, n_chunks;
   std::vector<fr_muon_coeffs> coeffs;
+  bool pair = false;
   uint32_t side = kMuonSmall;
   uint64_t scratch = 0;  // bytes
   fr_muon_info info{};
@@ -55,19 +56,23 @@ int check_shape(uint64_t rows, uint64_t cols) {
 // Whether the steps keep every singular value that starts in [0, 1], and the
 // polynomial's parts, inside what fp16 operands can hold with the powers of two
 // that they are stored times.
-int check_coeffs(const fr_muon_coeffs* c, uint32_t n, std::vector<fr_muon_coeffs>* out) {
-  if (!c) {
-    if (n) return FR_E_INVAL;
-    out->assign(5, kCoeffs);
-    return FR_OK;
-  }
-  if (n < 1 || n > FR_MUON_MAX_STEPS) return FR_E_INVAL;
-  out->assign(c, c + n);
+// *pair: those of the first two steps taken as one as well.
+int check_coeffs(const fr_muon_coeffs* c, uint32_t n, std::vector<fr_muon_coeffs>* out, bool* pair) {
+  if (!c && n) return FR_E_INVAL;
+  if (c && (n < 1 || n > FR_MUON_MAX_STEPS)) return FR_E_INVAL;
+  if (c) out->assign(c, c + n);
+  else out->assign(5, kCoeffs);
   for (const fr_muon_coeffs& k : *out)
     if (!std::isfinite(k.a) || !std::isfinite(k.b) || !std::isfinite(k.c)) return FR_E_INVAL;
+  *pair = out->size() >= 2;
   constexpr int kGrid = 4096;
   for (int i = 0; i <= kGrid; i++) {
     double s = double(i) / kGrid;
+    if (*pair) {
+      const fr_muon_coeffs &f = (*out)[0], &g = (*out)[1];
+      const double q = s * s, one = f.b * q + f.c * q * q, p = q * (f.a + one) * (f.a + one), two = g.b * p + g.c * p * p;
+      *pair = std::fabs(f.a * two) + std::fabs(g.a * one) + std::fabs(one * two) <= 64;
+    }
     for (const fr_muon_coeffs& k : *out) {
       const double q = s * s;
       if (std::fabs(k.b) * q + std::fabs(k.c) * q * q > 64) return FR_E_INVAL;
@@ -87,6 +92,7 @@ void lay_out_scratch(MuonLayout* out) {
   }
   out->side = large >= 256 ? kMuonLarge : kMuonSmall;
   for (MuonRec& r : out->recs) {
+    r.paired = out->pair && r.m >= kMuonPairedLess && r.n >= kMuonPairedMore;
     r.mp = uint32_t(up(r.m, out->side));
     r.np = uint32_t(up(r.n, out->side));
     if (!r.numel) continue;
@@ -94,8 +100,9 @@ void lay_out_scratch(MuonLayout* out) {
     const struct {
       uint64_t* where;
       uint64_t bytes;
-    } parts[7] = {{&r.x[0], 2 * wide}, {&r.x[1], 2 * wide}, {&r.rest, wide},     {&r.a, 2 * square},
-                  {&r.q, 2 * square},  {&r.da, 4ull * r.mp},  {&r.dq, 4ull * r.mp}};
+    } parts[9] = {{&r.x[0], 2 * wide},          {&r.x[1], 2 * wide},          {&r.rest, wide},
+                  {&r.square[0], 2 * square},   {&r.square[1], 2 * square},   {&r.square[2], 2 * square},
+                  {&r.diagonal[0], 4ull * r.mp}, {&r.diagonal[1], 4ull * r.mp}, {&r.diagonal[2], 4ull * r.mp}};
     for (const auto& p : parts) {
       *p.where = out->scratch;
       out->scratch += p.bytes;
@@ -107,7 +114,7 @@ int validate(const fr_tensor_desc* table, uint32_t n_entries, const Layout& L, u
              const fr_muon_tensor* t, uint32_t n, uint32_t n_groups, uint64_t grad_bytes, uint64_t update_bytes,
              const fr_muon_coeffs* coeffs, uint32_t n_steps, MuonLayout* out) {
   if (n && !t) return FR_E_INVAL;
-  FR_TRY(check_coeffs(coeffs, n_steps, &out->coeffs));
+  FR_TRY(check_coeffs(coeffs, n_steps, &out->coeffs, &out->pair));
   std::vector<uint8_t> named(n_entries, 0);
   std::vector<Range> written, updated;
   out->recs.resize(n);
@@ -256,7 +263,7 @@ int build(fr_muon* o) {
   const uint32_t n = uint32_t(Y.recs.size());
   std::vector<uint64_t> walk;
   std::vector<uint64_t> spread;
-  TileList gram, whole;
+  TileList gram[3], whole[3];
   std::vector<AdamwFold> mom, step;
   const bool sums = o->C >= FR_ADAMW_MIN_SUM_CHUNK;
   uint64_t slots = 0, subs = 0;
@@ -275,10 +282,12 @@ int build(fr_muon* o) {
     }
     if (!r.numel) continue;
     const uint32_t tm = r.mp / Y.side, tn = r.np / Y.side;
-    for (uint32_t i = 0; i < tm; i++)
-      for (uint32_t j = 0; j <= i; j++) gram.items.push_back({id | uint64_t(i) << 16 | j, r.np});
-    for (uint32_t j = 0; j < tn; j++)
-      for (uint32_t i = 0; i < tm; i++) whole.items.push_back({id | uint64_t(i) << 16 | j, r.mp});
+    for (uint32_t of : {r.paired, 2u}) {
+      for (uint32_t i = 0; i < tm; i++)
+        for (uint32_t j = 0; j <= i; j++) gram[of].items.push_back({id | uint64_t(i) << 16 | j, r.np});
+      for (uint32_t j = 0; j < tn; j++)
+        for (uint32_t i = 0; i < tm; i++) whole[of].items.push_back({id | uint64_t(i) << 16 | j, r.mp});
+    }
     for (uint64_t i = 0; i < uint64_t(r.mp) * r.np / 4096; i++) spread.push_back(id | i);
     if (!sums) continue;
     // chunk i of an array holds this many elements, and so these tiles
@@ -291,13 +300,21 @@ int build(fr_muon* o) {
         (j == 2 ? mom : step).push_back(f);
       }
   }
-  const std::vector<uint64_t> t_gram = gram.dealt(), t_whole = whole.dealt();
+  std::vector<uint64_t> t_gram[3], t_whole[3];
+  for (int i = 0; i < 3; i++) {
+    t_gram[i] = gram[i].dealt();
+    t_whole[i] = whole[i].dealt();
+  }
   Carver c;
   const size_t recs = c.add(Y.recs.data(), n * sizeof(MuonRec));
   const fr_grad_stats neutral = {0.0, 0.0f, 1.0f, 0};
   const size_t ns = c.add(&neutral, sizeof neutral);
   const size_t wa = c.add(walk.data(), walk.size() * 8);
-  const size_t tg = c.add(t_gram.data(), t_gram.size() * 8), tw = c.add(t_whole.data(), t_whole.size() * 8);
+  size_t tg[3], tw[3];
+  for (int i = 0; i < 3; i++) {
+    tg[i] = c.add(t_gram[i].data(), t_gram[i].size() * 8);
+    tw[i] = c.add(t_whole[i].data(), t_whole[i].size() * 8);
+  }
   const size_t ts = c.add(spread.data(), spread.size() * 8);
   const size_t fm = c.add(mom.data(), mom.size() * sizeof(AdamwFold));
   const size_t fs = c.add(step.data(), step.size() * sizeof(AdamwFold));
@@ -338,8 +355,10 @@ int build(fr_muon* o) {
   a.parts = reinterpret_cast<double*>(at(np));
   a.factors = reinterpret_cast<double*>(at(nf));
   a.spread = MuonTiles{reinterpret_cast<const uint64_t*>(at(ts)), spread.size()};
-  a.gram = MuonTiles{reinterpret_cast<const uint64_t*>(at(tg)), t_gram.size()};
-  a.whole = MuonTiles{reinterpret_cast<const uint64_t*>(at(tw)), t_whole.size()};
+  for (int i = 0; i < 3; i++) {
+    a.gram[i] = MuonTiles{reinterpret_cast<const uint64_t*>(at(tg[i])), t_gram[i].size()};
+    a.whole[i] = MuonTiles{reinterpret_cast<const uint64_t*>(at(tw[i])), t_whole[i].size()};
+  }
   a.coeffs = Y.coeffs.data();
   a.n_steps = uint32_t(Y.coeffs.size());
   o->mom_folds = reinterpret_cast<const AdamwFold*>(at(fm));

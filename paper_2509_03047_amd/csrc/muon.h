@@ -14,12 +14,12 @@ namespace fr {
 // and, for what the products read and write, the optimizer's scratch:
 //   x     mp x np, fp16    X, twice: read and written in turn
 //   rest  mp x np, 8 bits  what X is more than its fp16 number (e4m3)
-//   a, q  mp x mp, fp16    X X^T and the polynomial of it, with
-//   da, dq  mp, fp32       what their diagonals are more
+//   square    mp x mp, fp16   X X^T and polynomials of it, three at a time
+//   diagonal  mp, fp32        what their diagonals are more
 struct alignas(16) MuonRec {
   uint64_t numel;
   uint64_t grad, update, param, master, mom;  // param: kNone if it has none
-  uint64_t x[2], rest, a, q, da, dq;
+  uint64_t x[2], rest, square[3], diagonal[3];
   uint64_t slot0, slots;  // its tiles in the walk over elements
   uint64_t sub0;          // and its first sub-tile
   uint32_t cols, m, n, mp, np;
@@ -27,9 +27,10 @@ struct alignas(16) MuonRec {
   uint32_t grad_f32, group;
   float scale;
   float lift;         // the power of two that X is stored times
-  uint32_t pad_[2];
+  uint32_t paired;    // its first two steps are taken as one
+  uint32_t pad_;
 };
-static_assert(sizeof(MuonRec) == 176, "MuonRec is 176 bytes");
+static_assert(sizeof(MuonRec) == 192, "MuonRec is 192 bytes");
 
 // Elements of a workgroup of the walk over elements, and of those that make one
 // part of a chunk's sum.
@@ -37,6 +38,9 @@ constexpr uint32_t kMuonTile = 4096, kMuonSub = 1024;
 static_assert(kMuonSub * 4 <= FR_ADAMW_MIN_SUM_CHUNK, "a sub-tile lies inside a chunk");
 // Sides of the products' tiles, to which those of matrices are padded.
 constexpr uint32_t kMuonLarge = 256, kMuonSmall = 64;
+// Matrices whose first two steps are taken as one: five products of square
+// matrices more and one gram and one product with X less.
+constexpr uint32_t kMuonPairedLess = 128, kMuonPairedMore = 2048;
 constexpr float kMuonLiftA = 256.0f;  // A and Q are stored times this
 
 // A product's work: (matrix << 32) | (tile row << 16) | tile column, one for each
@@ -62,7 +66,9 @@ struct MuonArgs {
   void* updates = nullptr;
   bool momentum = false;   // of the state; else the gradients as they are
   MuonTiles spread;  // (matrix << 32) | tile of 4,096 elements
-  MuonTiles gram, whole;
+  // the products' of matrices whose first two steps are taken one by one, as one,
+  // and of all
+  MuonTiles gram[3], whole[3];
   const fr_muon_coeffs* coeffs = nullptr;
   uint32_t n_steps = 0;
   // sums, or sum_parts == NULL

@@ -93,6 +93,55 @@ def test_an_update_depends_on_its_matrix_alone(shape):
     assert np.array_equal(t.update(1, u), want) and np.array_equal(t.update(4, u), want)
 
 
+def orthogonalized_on_gpu(g, eps=1e-7, coeffs=R.STEPS):
+    """tests/muon_ref.py's, by fp64 products of the GPU."""
+    x = torch.from_numpy(g).cuda().double()
+    x = x / (torch.linalg.norm(x) + eps)
+    tall = x.shape[0] > x.shape[1]
+    x = x.t().contiguous() if tall else x
+    for a, b, c in np.asarray(coeffs, np.float32).astype(np.float64).tolist():
+        m = x @ x.t().contiguous()
+        x = a * x + (b * m + c * (m @ m)) @ x
+    return (x.t() if tall else x).cpu().numpy()
+
+
+LARGE = [(2048, 2048), (300, 2100), (2500, 140), (7, 9), (129, 5000), (1, 4000), (1500, 3), (2048, 2300), (2200, 2048),
+         (2048, 2048), (600, 700), (0, 3), (257, 2049)]
+
+
+@pytest.mark.parametrize("dtype", [F.FR_BF16, F.FR_F32])
+def test_large_tiles_and_two_steps_as_one(dtype):
+    """A list that takes tiles of 256 x 256: updates agree with 64 bits and have the bits that each matrix alone has,
+    whose products take tiles of 64 x 64; matrices whose first two steps are one are among them and others."""
+    s = R.Matrices(LARGE, dtype, seed=21)
+    tiles = sum(-(-a // 256) * -(-b // 256) for a, b in LARGE)
+    assert tiles >= 256  # else these are small tiles
+    u = Dev(s).orthogonalized()
+    for k, shape in enumerate(LARGE):
+        if not min(shape):
+            continue
+        want = orthogonalized_on_gpu(s.grad(k).reshape(shape))
+        e = off(s.update(k, u), want)
+        log(shape, f"{e:.2e}")
+        assert e <= tolerance(), shape
+        alone = R.Matrices([shape], dtype, seed=22)
+        alone.set_grad(0, s.grad(k))
+        assert np.array_equal(alone.update(0, Dev(alone).orthogonalized()), s.update(k, u)), shape
+    assert outside(s, u, 0xEE)
+
+
+@pytest.mark.parametrize("coeffs", [[(1.5, -0.5, 0.0)], [(1.5, -0.5, 0.0), (1.875, -1.25, 0.375)],
+                                    [(2.0, -1.5, 0.5)] * 3, [(3.4445, -4.775, 2.0315), (2.0, -1.5, 0.5)] * 4,
+                                    [(8.5, -34.0, 27.2), (8.8235, -12.2125, 3.3806)]])
+def test_other_steps_of_matrices_with_two_as_one(coeffs):
+    """Also of few steps, and where the first two may not be one (the last: their product's parts are too large)."""
+    s = R.Matrices([(130, 2050), (2050, 130), (64, 512)], F.FR_F32, seed=24)
+    u = Dev(s, coeffs=coeffs).orthogonalized()
+    for k, shape in enumerate(s.shapes):
+        want = R.orthogonalized(s.grad(k).reshape(shape), coeffs=coeffs)
+        assert off(s.update(k, u), want) <= tolerance(len(coeffs)), (shape, coeffs)
+
+
 @pytest.mark.parametrize("coeffs", [[(1.5, -0.5, 0.0)], [(1.5, -0.5, 0.0), (1.875, -1.25, 0.375)],
                                     [(2.0, -1.5, 0.5)] * 3, [(3.4445, -4.775, 2.0315), (2.0, -1.5, 0.5)] * 4,
                                     [(0.0, 0.0, 0.0)]])
