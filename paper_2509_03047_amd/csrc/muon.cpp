@@ -352,6 +352,8 @@ int build(fr_muon* o) {
   a.walk = AdamwWalk{reinterpret_cast<const uint64_t*>(at(wa)), slots, stride};
   a.scratch = at(sc);
   a.sub_stride = sub_stride;
+  a.few_slots = true;
+  for (const MuonRec& r : Y.recs) a.few_slots &= r.slots <= 256;
   a.parts = reinterpret_cast<double*>(at(np));
   a.factors = reinterpret_cast<double*>(at(nf));
   a.spread = MuonTiles{reinterpret_cast<const uint64_t*>(at(ts)), spread.size()};

@@ -57,6 +57,7 @@ struct MuonArgs {
   uint32_t units = 1;          // compute units, each of which takes one workgroup of large tiles
   AdamwWalk walk;          // tiles of kMuonTile elements
   uint8_t* scratch = nullptr;
+  bool few_slots = false;   // no matrix has more than 256 tiles in the walk
   double* parts = nullptr;  // a sum of squares for each place of the walk
   double* factors = nullptr; // of each matrix: lift / (|D| + eps)
   const fr_muon_hyper* hyper = nullptr;

@@ -220,20 +220,22 @@ __global__ __launch_bounds__(256) void k_muon_apply(MuonArgs a) {
   }
 }
 
-// A matrix's norm, and what its elements are multiplied by to be X_0 as it is
-// stored.  One workgroup a matrix.
-__global__ __launch_bounds__(256) void k_muon_norm(MuonArgs a) {
-  const MuonRec& r = a.recs[blockIdx.x];
+// What a matrix's elements are multiplied by to be X_0 as it is stored, from its
+// tiles' sums.  A workgroup's 256 threads take turns.
+__device__ __forceinline__ double factor_of(const MuonArgs& a, const MuonRec& r) {
   double q = 0;
   for (uint64_t i = threadIdx.x; i < r.slots; i += 256) {
     const uint64_t g = r.slot0 + i;
     q += a.parts[(g & 7) * a.walk.stride + (g >> 3)];
   }
   q = block_sum(q);
-  if (threadIdx.x == 0) {
-    const double f = double(r.lift) / (__builtin_sqrt(q) + double(a.hyper[r.group].eps));
-    a.factors[blockIdx.x] = q == 0.0 ? 0.0 : __builtin_isfinite(q) ? f : __builtin_nan("");
-  }
+  const double f = double(r.lift) / (__builtin_sqrt(q) + double(a.hyper[r.group].eps));
+  return q == 0.0 ? 0.0 : __builtin_isfinite(q) ? f : __builtin_nan("");
+}
+
+__global__ __launch_bounds__(256) void k_muon_norm(MuonArgs a) {
+  const double f = factor_of(a, a.recs[blockIdx.x]);
+  if (threadIdx.x == 0) a.factors[blockIdx.x] = f;
 }
 
 // ------------------------------------------------------------ X, as carried
@@ -301,6 +303,8 @@ __device__ __forceinline__ f32x4 spread_four(const MuonArgs& a, const MuonRec& r
   return d;
 }
 
+// kNorms: every workgroup takes its matrix's factor from the tiles' sums itself.
+template <bool kNorms>
 __global__ __launch_bounds__(256) void k_muon_spread(MuonArgs a) {
   if (a.stats->nonfinite) return;
   const uint64_t tile = a.spread.d[blockIdx.x];
@@ -309,7 +313,9 @@ __global__ __launch_bounds__(256) void k_muon_spread(MuonArgs a) {
   const bool flat = r.wide && r.np % 256 == 0;
   const uint32_t side = flat ? 256 : 64, across = r.np / side;
   const uint32_t i0 = uint32_t(tile) / across * (4096 / side), j0 = uint32_t(tile) % across * side;
-  const double f = a.factors[id];
+  double f;
+  if constexpr (kNorms) f = factor_of(a, r);
+  else f = a.factors[id];
   const fr_muon_hyper h = a.hyper[r.group];
   const float scale = a.stats->scale;
   f16* const x = reinterpret_cast<f16*>(a.scratch + r.x[0]);
@@ -595,11 +601,41 @@ struct Mirror {
   }
 };
 
+// What a pair's sum is added to, of two times 16 rows: L and R there, and what
+// their diagonals are more.
+template <class T>
+struct Terms {
+  static constexpr uint32_t N = T::WN / 16;
+  f16x8 x[2][N / 2], y[2][N / 2];
+  f32x4 ej[N / 2][2];
+  float ei[2];
+  __device__ __forceinline__ void load(const ProductArgs& args, const MuonRec& rec, const Product& p, uint32_t i,
+                                       uint32_t j) {
+    const f16* const L = reinterpret_cast<const f16*>(args.scratch + rec.square[p.l]);
+    const f16* const R = reinterpret_cast<const f16*>(args.scratch + rec.square[p.r]);
+    const float* const dl = reinterpret_cast<const float*>(args.scratch + rec.diagonal[p.l]);
+    const float* const dr = reinterpret_cast<const float*>(args.scratch + rec.diagonal[p.r]);
+#pragma unroll
+    for (uint32_t s = 0; s < 2; s++) {
+      ei[s] = dl[i + 16 * s];
+#pragma unroll
+      for (uint32_t c = 0; c < N / 2; c++) {
+        x[s][c] = *reinterpret_cast<const f16x8*>(L + uint64_t(i + 16 * s) * rec.mp + j + 32 * c);
+        y[s][c] = *reinterpret_cast<const f16x8*>(R + uint64_t(i + 16 * s) * rec.mp + j + 32 * c);
+      }
+    }
+#pragma unroll
+    for (uint32_t c = 0; c < N / 2; c++)
+#pragma unroll
+      for (uint32_t k = 0; k < 2; k++) ej[c][k] = *reinterpret_cast<const f32x4*>(dr + j + 32 * c + 4 * k);
+  }
+};
+
 // Tiles of L R (kWhole, with R's columns along the sum) or L R^T, one after
 // another: the next one's first slices are loaded while one's results are stored.
 template <MuonProduct kWhat, class T>
 __global__ __launch_bounds__(T::threads) void k_muon_product(ProductArgs args) {
-  if (args.stats->nonfinite) return;
+  const bool skip = args.stats->nonfinite != 0;  // (on its way together with the tile)
   extern __shared__ __attribute__((aligned(16))) f16 lds[];
   constexpr uint32_t kSlice = Lds<T>::slice, M = T::WM / 16, N = T::WN / 16;
   constexpr uint32_t kLoads = 2 * kSlice / (8 * T::threads);  // of a wave, a slice of both operands
@@ -608,6 +644,7 @@ __global__ __launch_bounds__(T::threads) void k_muon_product(ProductArgs args) {
   const Mirror<T> mirror(lds, wave);
   typedef Place<kWhat, T> Here;
   Here here = Here::of(args, blockIdx.x, wave);
+  if (skip) return;
   f32x4 acc[M][N];
   typedef Operands<T, kWhat == kWhole> Ops;
   Ops o{wi, wj};
@@ -724,6 +761,13 @@ __global__ __launch_bounds__(T::threads) void k_muon_product(ProductArgs args) {
 #pragma unroll
         for (uint32_t q = 0; q < N; q++) acc[s][q] = f32x4{0, 0, 0, 0};
     }
+    // Of small tiles, what a pair's sum is added to comes before the sum; large ones
+    // have no registers for it.
+    constexpr bool kEarly = kWhat == kPair && T::B == kMuonSmall;
+    Terms<T> early[kEarly ? M / 2 : 1];
+    if constexpr (kEarly)
+#pragma unroll
+      for (uint32_t b = 0; b < M / 2; b++) early[b].load(args, *here.rec, p, i1 + 32 * b, j1);
     const uint32_t K = here.K;
     if (T::S * T::D <= K) arrive<(T::S - 1) * kLoads>();
     else arrive<0>();
@@ -824,36 +868,16 @@ __global__ __launch_bounds__(T::threads) void k_muon_product(ProductArgs args) {
       // out: what it leaves is kept, and counts in what follows.  With those of L
       // and R, l and r, a product is L R + diag(l) R + L diag(r) of the fp16 ones
       // (but for l r).
-      const f16* const L = reinterpret_cast<const f16*>(args.scratch + rec->square[p.l]);
-      const f16* const R = reinterpret_cast<const f16*>(args.scratch + rec->square[p.r]);
-      const float* const dl = reinterpret_cast<const float*>(args.scratch + rec->diagonal[p.l]);
-      const float* const dr = reinterpret_cast<const float*>(args.scratch + rec->diagonal[p.r]);
       f16* const out = reinterpret_cast<f16*>(args.scratch + rec->square[p.out]);
       float* const left = reinterpret_cast<float*>(args.scratch + rec->diagonal[p.out]);
       const uint32_t ld = rec->mp;
       const float scale = kWhat == kGram ? kMuonLiftA / (rec->lift * rec->lift) : p.w * (1.0f / kMuonLiftA);
-      f32x4 ej[N / 2][2];
-      if constexpr (kWhat == kPair)
-#pragma unroll
-        for (uint32_t c = 0; c < N / 2; c++)
-#pragma unroll
-          for (uint32_t k = 0; k < 2; k++) ej[c][k] = *reinterpret_cast<const f32x4*>(dr + j1 + 32 * c + 4 * k);
 #pragma unroll
       for (uint32_t b = 0; b < M / 2; b++) {
         asm volatile("" ::: "memory");
-        f16x8 x[2][N / 2], y[2][N / 2];
-        float ei[2];
-        if constexpr (kWhat == kPair)
-#pragma unroll
-          for (uint32_t s = 0; s < 2; s++) {
-            const uint32_t i = i1 + 16 * (2 * b + s);
-            ei[s] = dl[i];
-#pragma unroll
-            for (uint32_t c = 0; c < N / 2; c++) {
-              x[s][c] = *reinterpret_cast<const f16x8*>(L + uint64_t(i) * ld + j1 + 32 * c);
-              y[s][c] = *reinterpret_cast<const f16x8*>(R + uint64_t(i) * ld + j1 + 32 * c);
-            }
-          }
+        Terms<T> terms;
+        if constexpr (kEarly) terms = early[b];
+        else if constexpr (kWhat == kPair) terms.load(args, *rec, p, i1 + 32 * b, j1);
 #pragma unroll
         for (uint32_t s = 2 * b; s < 2 * b + 2; s++)
 #pragma unroll
@@ -865,9 +889,9 @@ __global__ __launch_bounds__(T::threads) void k_muon_product(ProductArgs args) {
               float v = scale * acc[s][2 * c + e / 4][e % 4];
               const bool on = diagonal && i == j + e;
               if constexpr (kWhat == kPair) {
-                const float er = ej[c][e / 4][e % 4], el = ei[s % 2];
-                v = __builtin_fmaf(__builtin_fmaf(scale, er, p.u), float(x[s % 2][c][e]), v);
-                v = __builtin_fmaf(__builtin_fmaf(scale, el, p.v), float(y[s % 2][c][e]), v);
+                const float er = terms.ej[c][e / 4][e % 4], el = terms.ei[s % 2];
+                v = __builtin_fmaf(__builtin_fmaf(scale, er, p.u), float(terms.x[s % 2][c][e]), v);
+                v = __builtin_fmaf(__builtin_fmaf(scale, el, p.v), float(terms.y[s % 2][c][e]), v);
                 if (on) v = __builtin_fmaf(p.u, el, __builtin_fmaf(p.v, er, v));
               }
               h[e] = f16(v);
@@ -1001,9 +1025,13 @@ int launch_muon_direction(const MuonArgs& a, void* stream) {
   else hipLaunchKernelGGL((k_muon_momentum<true, false>), tiles, dim3(256), 0, st, a);
   if (const int e = int(hipGetLastError())) return e;
   if (const int e = fold(a, st)) return e;
-  hipLaunchKernelGGL(k_muon_norm, dim3(a.n), dim3(256), 0, st, a);
-  if (const int e = int(hipGetLastError())) return e;
-  hipLaunchKernelGGL(k_muon_spread, dim3(uint32_t(a.spread.n)), dim3(256), 0, st, a);
+  if (a.few_slots) {
+    hipLaunchKernelGGL(k_muon_spread<true>, dim3(uint32_t(a.spread.n)), dim3(256), 0, st, a);
+  } else {
+    hipLaunchKernelGGL(k_muon_norm, dim3(a.n), dim3(256), 0, st, a);
+    if (const int e = int(hipGetLastError())) return e;
+    hipLaunchKernelGGL(k_muon_spread<false>, dim3(uint32_t(a.spread.n)), dim3(256), 0, st, a);
+  }
   if (const int e = int(hipGetLastError())) return e;
   return a.side == kMuonLarge ? products<Large>(a, st) : products<Small>(a, st);
 }
