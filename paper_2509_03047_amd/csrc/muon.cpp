@@ -242,17 +242,18 @@ struct Carver {
 struct TileList {
   static constexpr size_t kRun = 16;
   struct Item {
-    uint64_t tile;
+    uint64_t tile;  // (matrix << 32) | (row << 16) | column
     uint32_t k;
   };
   std::vector<Item> items;
-  std::vector<uint64_t> dealt() {
+  std::vector<MuonTile> dealt(const std::vector<MuonRec>& recs, uint32_t side) {
     std::stable_sort(items.begin(), items.end(), [](const Item& a, const Item& b) { return a.k > b.k; });
     const size_t n = items.size(), whole = n / (8 * kRun) * (8 * kRun);
-    std::vector<uint64_t> d(n);
+    std::vector<MuonTile> d(n);
     for (size_t b = 0; b < n; b++) {
       const size_t i = b % (8 * kRun);
-      d[b] = items[b < whole ? b - i + i % 8 * kRun + i / 8 : b].tile;
+      const uint64_t t = items[b < whole ? b - i + i % 8 * kRun + i / 8 : b].tile;
+      d[b] = MuonTile{recs[t >> 32], uint32_t(t >> 16 & 0xFFFF) * side, uint32_t(t & 0xFFFF) * side, 0};
     }
     return d;
   }
@@ -300,10 +301,10 @@ int build(fr_muon* o) {
         (j == 2 ? mom : step).push_back(f);
       }
   }
-  std::vector<uint64_t> t_gram[3], t_whole[3];
+  std::vector<MuonTile> t_gram[3], t_whole[3];
   for (int i = 0; i < 3; i++) {
-    t_gram[i] = gram[i].dealt();
-    t_whole[i] = whole[i].dealt();
+    t_gram[i] = gram[i].dealt(Y.recs, Y.side);
+    t_whole[i] = whole[i].dealt(Y.recs, Y.side);
   }
   Carver c;
   const size_t recs = c.add(Y.recs.data(), n * sizeof(MuonRec));
@@ -312,8 +313,8 @@ int build(fr_muon* o) {
   const size_t wa = c.add(walk.data(), walk.size() * 8);
   size_t tg[3], tw[3];
   for (int i = 0; i < 3; i++) {
-    tg[i] = c.add(t_gram[i].data(), t_gram[i].size() * 8);
-    tw[i] = c.add(t_whole[i].data(), t_whole[i].size() * 8);
+    tg[i] = c.add(t_gram[i].data(), t_gram[i].size() * sizeof(MuonTile));
+    tw[i] = c.add(t_whole[i].data(), t_whole[i].size() * sizeof(MuonTile));
   }
   const size_t ts = c.add(spread.data(), spread.size() * 8);
   const size_t fm = c.add(mom.data(), mom.size() * sizeof(AdamwFold));
@@ -356,10 +357,11 @@ int build(fr_muon* o) {
   for (const MuonRec& r : Y.recs) a.few_slots &= r.slots <= 256;
   a.parts = reinterpret_cast<double*>(at(np));
   a.factors = reinterpret_cast<double*>(at(nf));
-  a.spread = MuonTiles{reinterpret_cast<const uint64_t*>(at(ts)), spread.size()};
+  a.spread = reinterpret_cast<const uint64_t*>(at(ts));
+  a.n_spread = spread.size();
   for (int i = 0; i < 3; i++) {
-    a.gram[i] = MuonTiles{reinterpret_cast<const uint64_t*>(at(tg[i])), t_gram[i].size()};
-    a.whole[i] = MuonTiles{reinterpret_cast<const uint64_t*>(at(tw[i])), t_whole[i].size()};
+    a.gram[i] = MuonTiles{reinterpret_cast<const MuonTile*>(at(tg[i])), t_gram[i].size()};
+    a.whole[i] = MuonTiles{reinterpret_cast<const MuonTile*>(at(tw[i])), t_whole[i].size()};
   }
   a.coeffs = Y.coeffs.data();
   a.n_steps = uint32_t(Y.coeffs.size());

@@ -43,10 +43,16 @@ constexpr uint32_t kMuonLarge = 256, kMuonSmall = 64;
 constexpr uint32_t kMuonPairedLess = 128, kMuonPairedMore = 2048;
 constexpr float kMuonLiftA = 256.0f;  // A and Q are stored times this
 
-// A product's work: (matrix << 32) | (tile row << 16) | tile column, one for each
-// workgroup.
+// A product's work, one entry for each workgroup: a tile of a matrix, of which it
+// has a copy (a chain of loads less: of a few small matrices a product takes 5 to 9
+// us, most of it such chains).
+struct alignas(16) MuonTile {
+  MuonRec rec;
+  uint32_t i0, j0;
+  uint64_t pad_;
+};
 struct MuonTiles {
-  const uint64_t* d = nullptr;
+  const MuonTile* d = nullptr;
   uint64_t n = 0;
 };
 
@@ -66,7 +72,8 @@ struct MuonArgs {
   const void* grads = nullptr;
   void* updates = nullptr;
   bool momentum = false;   // of the state; else the gradients as they are
-  MuonTiles spread;  // (matrix << 32) | tile of 4,096 elements
+  const uint64_t* spread = nullptr;  // (matrix << 32) | tile of 4,096 elements
+  uint64_t n_spread = 0;
   // the products' of matrices whose first two steps are taken one by one, as one,
   // and of all
   MuonTiles gram[3], whole[3];

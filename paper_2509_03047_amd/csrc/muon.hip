@@ -307,7 +307,7 @@ __device__ __forceinline__ f32x4 spread_four(const MuonArgs& a, const MuonRec& r
 template <bool kNorms>
 __global__ __launch_bounds__(256) void k_muon_spread(MuonArgs a) {
   if (a.stats->nonfinite) return;
-  const uint64_t tile = a.spread.d[blockIdx.x];
+  const uint64_t tile = a.spread[blockIdx.x];
   const uint32_t id = uint32_t(tile >> 32);
   const MuonRec r = a.recs[id];
   const bool flat = r.wide && r.np % 256 == 0;
@@ -351,23 +351,23 @@ __global__ __launch_bounds__(256) void k_muon_spread(MuonArgs a) {
 
 // ------------------------------------------------------------------ products
 
-// A = X X^T; polynomials of it from two that are there; the next X = a X + P X.
-enum MuonProduct { kGram, kPair, kWhole };
+// A = X X^T; polynomials of it from one that is there, or from two; the next X =
+// a X + P X.
+enum MuonProduct { kGram, kSquare, kPair, kWhole };
 
 // What a launch does.
 struct Product {
   // of the square ones, which are read (one by kWhole) and which is written
   uint32_t l, r, out;
-  float u, v, w;     // kPair: u L + v R + w L R; kWhole: u X + L X
+  float u, v, w;     // kSquare: u L + w L L; kPair: u L + v R + w L R; kWhole: u X + L X
   uint32_t flip;     // which X is read; the other is written
   uint32_t carried;  // X has a rest
   uint32_t carry;    // and gets one
   uint32_t last;
 };
 struct ProductArgs {
-  const MuonRec* recs;
-  const uint64_t* tiles;
-  uint32_t n;  // tiles
+  const MuonTile* tiles;
+  uint32_t n;
   uint8_t* scratch;
   uint8_t* updates;
   const fr_grad_stats* stats;
@@ -523,6 +523,36 @@ struct Operands {
   }
 };
 
+// All of a slice's operands at once, of a wave with few.
+template <class T, bool kColumns>
+struct SliceOperands {
+  static constexpr uint32_t M = T::WM / 16, N = T::WN / 16;
+  f16x8 y[T::D / 32][N], x[T::D / 32][M];
+  __device__ __forceinline__ void read(const f16* lds, uint32_t wi, uint32_t wj) {
+    const uint32_t lane = threadIdx.x % 64;
+    const f16* const r = lds + T::B * T::D;
+#pragma unroll
+    for (uint32_t kk = 0; kk < T::D / 32; kk++) {
+#pragma unroll
+      for (uint32_t q = 0; q < N; q++)
+        y[kk][q] = kColumns ? operand_of_columns<T>(r, wj, q, kk)
+                            : operand_of_row<T, true>(r, wj + column_of(q, lane % 16), kk * 4 + lane / 16);
+#pragma unroll
+      for (uint32_t s = 0; s < M; s++)
+        x[kk][s] = operand_of_row<T, false>(lds, wi + s * 16 + lane % 16, kk * 4 + lane / 16);
+    }
+  }
+  __device__ __forceinline__ void multiply(f32x4 (&acc)[M][N]) const {
+#pragma unroll
+    for (uint32_t kk = 0; kk < T::D / 32; kk++)
+#pragma unroll
+      for (uint32_t s = 0; s < M; s++)
+#pragma unroll
+        for (uint32_t q = 0; q < N; q++)
+          acc[s][q] = __builtin_amdgcn_mfma_f32_16x16x32_f16(y[kk][q], x[kk][s], acc[s][q], 0, 0, 0);
+  }
+};
+
 // The order of what stands before it: one of kReads reads of LDS, then its share
 // of kProducts matrix instructions.
 template <uint32_t kReads, uint32_t kProducts>
@@ -555,14 +585,16 @@ struct Place {
   Rows<T, false> left;
   std::conditional_t<kWhat == kWhole, Columns<T>, Rows<T, true>> right;
   static __device__ __forceinline__ Place of(const ProductArgs& args, uint32_t t, uint32_t wave) {
-    const uint64_t tile = args.tiles[t];
-    const MuonRec* const rec = args.recs + (tile >> 32);
+    const MuonTile& tile = args.tiles[t];
+    const MuonRec* const rec = &tile.rec;
     const Product& p = args.of[rec->paired];
-    const uint32_t i0 = uint32_t(tile >> 16 & 0xFFFF) * T::B, j0 = uint32_t(tile & 0xFFFF) * T::B;
     const uint32_t K = kWhat == kGram ? rec->np : rec->mp, ld = kWhat == kWhole ? rec->np : K;
     const f16* const X = reinterpret_cast<const f16*>(args.scratch + rec->x[p.flip]);
     const f16* const L = kWhat == kGram ? X : reinterpret_cast<const f16*>(args.scratch + rec->square[p.l]);
-    const f16* const R = kWhat == kPair ? reinterpret_cast<const f16*>(args.scratch + rec->square[p.r]) : X;
+    const f16* const R = kWhat == kPair     ? reinterpret_cast<const f16*>(args.scratch + rec->square[p.r])
+                         : kWhat == kSquare ? L
+                                            : X;
+    const uint32_t i0 = tile.i0, j0 = tile.j0;
     return Place{rec, i0, j0, K, ld, L + uint64_t(i0) * K, kWhat == kWhole ? R + j0 : R + uint64_t(j0) * K,
                  {wave, K}, {wave, ld}};
   }
@@ -601,27 +633,28 @@ struct Mirror {
   }
 };
 
-// What a pair's sum is added to, of two times 16 rows: L and R there, and what
-// their diagonals are more.
-template <class T>
+// What a sum of kSquare or (kTwo) kPair is added to, of two times 16 rows: L and R
+// there, and what their diagonals are more.
+template <class T, bool kTwo>
 struct Terms {
   static constexpr uint32_t N = T::WN / 16;
-  f16x8 x[2][N / 2], y[2][N / 2];
+  f16x8 x[2][N / 2], y[kTwo ? 2 : 1][kTwo ? N / 2 : 1];
   f32x4 ej[N / 2][2];
   float ei[2];
   __device__ __forceinline__ void load(const ProductArgs& args, const MuonRec& rec, const Product& p, uint32_t i,
                                        uint32_t j) {
     const f16* const L = reinterpret_cast<const f16*>(args.scratch + rec.square[p.l]);
-    const f16* const R = reinterpret_cast<const f16*>(args.scratch + rec.square[p.r]);
+    const f16* const R = reinterpret_cast<const f16*>(args.scratch + rec.square[kTwo ? p.r : p.l]);
     const float* const dl = reinterpret_cast<const float*>(args.scratch + rec.diagonal[p.l]);
-    const float* const dr = reinterpret_cast<const float*>(args.scratch + rec.diagonal[p.r]);
+    const float* const dr = reinterpret_cast<const float*>(args.scratch + rec.diagonal[kTwo ? p.r : p.l]);
 #pragma unroll
     for (uint32_t s = 0; s < 2; s++) {
       ei[s] = dl[i + 16 * s];
 #pragma unroll
       for (uint32_t c = 0; c < N / 2; c++) {
         x[s][c] = *reinterpret_cast<const f16x8*>(L + uint64_t(i + 16 * s) * rec.mp + j + 32 * c);
-        y[s][c] = *reinterpret_cast<const f16x8*>(R + uint64_t(i + 16 * s) * rec.mp + j + 32 * c);
+        if constexpr (kTwo)
+          y[s][c] = *reinterpret_cast<const f16x8*>(R + uint64_t(i + 16 * s) * rec.mp + j + 32 * c);
       }
     }
 #pragma unroll
@@ -761,28 +794,47 @@ __global__ __launch_bounds__(T::threads) void k_muon_product(ProductArgs args) {
 #pragma unroll
         for (uint32_t q = 0; q < N; q++) acc[s][q] = f32x4{0, 0, 0, 0};
     }
-    // Of small tiles, what a pair's sum is added to comes before the sum; large ones
-    // have no registers for it.
-    constexpr bool kEarly = kWhat == kPair && T::B == kMuonSmall;
-    Terms<T> early[kEarly ? M / 2 : 1];
+    // Of small tiles, what a sum is added to comes before it; large ones have no
+    // registers for it.
+    constexpr bool kTwo = kWhat == kPair, kAdds = kTwo || kWhat == kSquare, kEarly = kAdds && T::B == kMuonSmall;
+    Terms<T, kTwo> early[kEarly ? M / 2 : 1];
     if constexpr (kEarly)
 #pragma unroll
       for (uint32_t b = 0; b < M / 2; b++) early[b].load(args, *here.rec, p, i1 + 32 * b, j1);
     const uint32_t K = here.K;
     if (T::S * T::D <= K) arrive<(T::S - 1) * kLoads>();
     else arrive<0>();
-    o.read_r(0, at, 0);
-    o.read_l(0, at, 0);
-    uint32_t k = 0;
-    for (; k + 64 - T::D + T::S * T::D < K; k += 64) sixty_four(k, yes, yes, no);
-    if constexpr (T::D == 32 && T::S % 2 == 1) {
-      if (k + T::S * T::D < K) {
-        sixty_four(k, yes, no, no);
-        k += 64;
+    if constexpr (T::B == kMuonSmall) {
+      SliceOperands<T, kWhat == kWhole> even, odd;
+      even.read(at, wi, wj);
+      // the next slice is read while one is multiplied; whether there was one
+      const auto slice = [&](uint32_t k, const auto& one, auto& other) {
+        const bool next = k + T::D < K;
+        if (next) {
+          if (k + T::S * T::D <= K) arrive<(T::S - 2) * kLoads>();
+          else arrive<0>();
+          if (k + T::S * T::D < K) fetch(k + T::S * T::D);
+          at = following(at);
+          other.read(at, wi, wj);
+        }
+        one.multiply(acc);
+        return next;
+      };
+      for (uint32_t k = 0; slice(k, even, odd) && slice(k + T::D, odd, even);) k += 2 * T::D;
+    } else {
+      o.read_r(0, at, 0);
+      o.read_l(0, at, 0);
+      uint32_t k = 0;
+      for (; k + 64 - T::D + T::S * T::D < K; k += 64) sixty_four(k, yes, yes, no);
+      if constexpr (T::D == 32 && T::S % 2 == 1) {
+        if (k + T::S * T::D < K) {
+          sixty_four(k, yes, no, no);
+          k += 64;
+        }
       }
+      for (; k + 64 < K; k += 64) sixty_four(k, no, no, no);
+      sixty_four(k, no, no, yes);
     }
-    for (; k + 64 < K; k += 64) sixty_four(k, no, no, no);
-    sixty_four(k, no, no, yes);
 
     const MuonRec* const rec = here.rec;
     const bool diagonal = here.i0 == here.j0;
@@ -871,13 +923,16 @@ __global__ __launch_bounds__(T::threads) void k_muon_product(ProductArgs args) {
       f16* const out = reinterpret_cast<f16*>(args.scratch + rec->square[p.out]);
       float* const left = reinterpret_cast<float*>(args.scratch + rec->diagonal[p.out]);
       const uint32_t ld = rec->mp;
+      // Of one operand, the product is symmetric to the last bit; of two, what is on
+      // and below the diagonal counts on both sides.
+      const bool halves = kTwo && diagonal;
       const float scale = kWhat == kGram ? kMuonLiftA / (rec->lift * rec->lift) : p.w * (1.0f / kMuonLiftA);
 #pragma unroll
       for (uint32_t b = 0; b < M / 2; b++) {
         asm volatile("" ::: "memory");
-        Terms<T> terms;
+        Terms<T, kTwo> terms;
         if constexpr (kEarly) terms = early[b];
-        else if constexpr (kWhat == kPair) terms.load(args, *rec, p, i1 + 32 * b, j1);
+        else if constexpr (kAdds) terms.load(args, *rec, p, i1 + 32 * b, j1);
 #pragma unroll
         for (uint32_t s = 2 * b; s < 2 * b + 2; s++)
 #pragma unroll
@@ -888,18 +943,22 @@ __global__ __launch_bounds__(T::threads) void k_muon_product(ProductArgs args) {
             for (uint32_t e = 0; e < 8; e++) {
               float v = scale * acc[s][2 * c + e / 4][e % 4];
               const bool on = diagonal && i == j + e;
-              if constexpr (kWhat == kPair) {
+              if constexpr (kAdds) {
                 const float er = terms.ej[c][e / 4][e % 4], el = terms.ei[s % 2];
-                v = __builtin_fmaf(__builtin_fmaf(scale, er, p.u), float(terms.x[s % 2][c][e]), v);
-                v = __builtin_fmaf(__builtin_fmaf(scale, el, p.v), float(terms.y[s % 2][c][e]), v);
-                if (on) v = __builtin_fmaf(p.u, el, __builtin_fmaf(p.v, er, v));
+                if constexpr (kTwo) {
+                  v = __builtin_fmaf(__builtin_fmaf(scale, er, p.u), float(terms.x[s % 2][c][e]), v);
+                  v = __builtin_fmaf(__builtin_fmaf(scale, el, p.v), float(terms.y[s % 2][c][e]), v);
+                  if (on) v = __builtin_fmaf(p.u, el, __builtin_fmaf(p.v, er, v));
+                } else {
+                  v = __builtin_fmaf(__builtin_fmaf(scale, el + er, p.u), float(terms.x[s % 2][c][e]), v);
+                  if (on) v = __builtin_fmaf(p.u, el, v);
+                }
               }
               h[e] = f16(v);
               if (on) left[i] = v - float(h[e]);
             }
-            // of a tile on the diagonal, what is on and below it
             f16* const to = out + uint64_t(i) * ld + j;
-            if (!diagonal || j + 7 <= i) {
+            if (!halves || j + 7 <= i) {
               *reinterpret_cast<f16x8*>(to) = h;
             } else {
 #pragma unroll
@@ -908,15 +967,14 @@ __global__ __launch_bounds__(T::threads) void k_muon_product(ProductArgs args) {
             }
             mirror.write(s % 2, c, h);
           }
+        if (diagonal && !halves) continue;
         asm volatile("" ::: "memory");
-        // and the same above it (of two different operands neither half is computed
-        // to the same bits)
 #pragma unroll
         for (uint32_t q = 0; q < N; q++) {
           const u32x4 h = mirror.read(q);
           const uint32_t i = i2 + q * 16, j = j2 + 32 * b;
           f16* const to = out + uint64_t(i) * ld + j;
-          if (!diagonal || j > i) {
+          if (!halves || j > i) {
             *reinterpret_cast<u32x4*>(to) = h;
           } else {
 #pragma unroll
@@ -934,7 +992,6 @@ template <class T>
 int products(const MuonArgs& a, hipStream_t st) {
   enum { kStep, kPaired, kAll };  // which matrices
   ProductArgs p;
-  p.recs = a.recs;
   p.scratch = a.scratch;
   p.updates = static_cast<uint8_t*>(a.updates);
   p.stats = a.stats;
@@ -960,7 +1017,8 @@ int products(const MuonArgs& a, hipStream_t st) {
       x.v = v;
       x.w = w;
     }
-    return launch(k_muon_product<kPair, T>, a.gram[which]);
+    return l == r ? launch(k_muon_product<kSquare, T>, a.gram[which])
+                  : launch(k_muon_product<kPair, T>, a.gram[which]);
   };
   // X goes from step `s` on up to `next`, by u X + L X
   const auto set_whole = [&](Product& x, uint32_t l, float u, uint32_t s, uint32_t next) {
@@ -1026,11 +1084,11 @@ int launch_muon_direction(const MuonArgs& a, void* stream) {
   if (const int e = int(hipGetLastError())) return e;
   if (const int e = fold(a, st)) return e;
   if (a.few_slots) {
-    hipLaunchKernelGGL(k_muon_spread<true>, dim3(uint32_t(a.spread.n)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(k_muon_spread<true>, dim3(uint32_t(a.n_spread)), dim3(256), 0, st, a);
   } else {
     hipLaunchKernelGGL(k_muon_norm, dim3(a.n), dim3(256), 0, st, a);
     if (const int e = int(hipGetLastError())) return e;
-    hipLaunchKernelGGL(k_muon_spread<false>, dim3(uint32_t(a.spread.n)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(k_muon_spread<false>, dim3(uint32_t(a.n_spread)), dim3(256), 0, st, a);
   }
   if (const int e = int(hipGetLastError())) return e;
   return a.side == kMuonLarge ? products<Large>(a, st) : products<Small>(a, st);
