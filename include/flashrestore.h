@@ -658,13 +658,14 @@ int fr_adamw_convert(const fr_adamw* from, const void* from_state, const fr_adam
  *       X_(i+1) = a_i X_i + (b_i A + c_i A A) X_i,  A = X_i X_i^T
  *     (with X_i^T X_i on the right where rows > cols) over the optimizer's
  *     steps; the update U is the last X in bf16.  On singular values a step is
- *     the polynomial a s + b s^3 + c s^5.  The sum of squares is kept in 64 bits,
+ *     the polynomial a s + b s^3 + c s^5.  The sum of squares is kept in 64 bits;
  *     products have fp16 operands (a power of two brings them into its range)
- *     and fp32 sums; X itself is carried in fp32 up to the last step but two.
- *     The updates differ from the exact ones by some 2e-3 of their norm, of
- *     which bf16 alone makes 1.7e-3.  U depends on D, eps and the coefficients
- *     alone, not on the other matrices nor on the launch: replicas stay
- *     identical bit for bit.
+ *     and fp32 sums; X has up to four bits more while three or more steps are to
+ *     come, and what fp16 leaves of the diagonals of A and of its polynomials is
+ *     kept and counted.  Updates are then off by some 1.8e-3 of their norm (those
+ *     of a few elements up to 3e-3), of which the rounding to bf16 makes 1.7e-3.  U depends on D, eps and the
+ *     coefficients alone, not on the other matrices nor on the launch: replicas
+ *     stay identical bit for bit.
  *     A matrix of zeros gives zeros (eps > 0); one that holds a NaN or an
  *     infinity gives NaN everywhere; other matrices do not feel it.
  *   Step, rounded operation by operation like AdamW's, with the matrix's scale:
@@ -714,9 +715,11 @@ typedef struct fr_muon_info {
   uint64_t update_arena_bytes;
   uint64_t arena_bytes;        /* of the state: the plan's src_arena_bytes */
   uint64_t sums_chunks;        /* chunks whose sums direction and apply write */
-  uint64_t device_bytes;       /* device memory of the optimizer itself, some 10
-                                  bytes an element and 4 for each of a product's
-                                  (0 for a query) */
+  uint64_t device_bytes;       /* device memory of the optimizer itself: 5 bytes for
+                                  each element and 6 for each of the smaller
+                                  sides' squares, sides rounded up to 64 (256 for
+                                  256 or more tiles of 256 x 256 in all) (0 for a
+                                  query) */
   int64_t device;              /* -1 for a query */
 } fr_muon_info;
 
@@ -730,8 +733,9 @@ typedef struct fr_muon_info {
  * master's numel, a scale that is not finite, and coefficients that are not
  * finite or let a singular value in [0, 1] grow past 4, or |b s^2| + |c s^4|
  * past 64, on the way; FR_E_RANGE for a side of more than 2^20 or 2^31 elements
- * or more, a smaller side above 2^15, 2^34 elements in all; FR_E_OVERLAP also for
- * two updates that overlap.
+ * or more, a smaller side above 2^15, and for 2^34 elements in all, those of a
+ * matrix counted in whole 4,096s, or 2^35 with sides rounded up to 64;
+ * FR_E_OVERLAP also for two updates that overlap.
  *   The plan need not outlive the optimizer.  Synchronous; create optimizers
  * outside graph capture. */
 int fr_muon_create(const fr_plan* plan, const fr_muon_tensor* tensors, uint32_t n, uint32_t n_groups,
@@ -767,6 +771,11 @@ int fr_muon_state_table(const uint32_t* shapes, uint32_t n, uint32_t grad_dtype,
  * overlap.  `sums` as in fr_adamw_step; a call writes those of the entries that
  * it writes.  stats: NULL (scale 1), or with nonfinite set a call changes
  * neither state nor updates (sums are those of the state as it is). */
+
+/* As fr_grad_norm, of the matrices' gradients.  For a norm over those of an
+ * fr_adamw as well, add up their sum_sq and call fr_grad_scale. */
+int fr_muon_grad_norm(const fr_muon* opt, const void* grads, float max_norm, fr_grad_stats* stats,
+                      hipStream_t stream);
 
 /* Momenta of the state and updates <- the next ones.
  *   state    device, 16-byte aligned, the plan's src_arena_bytes

@@ -217,6 +217,7 @@ struct fr_muon {
   uint32_t n_mom_folds = 0, n_step_folds = 0;
   fr_chunk_sum* sum_parts = nullptr;
   const fr_grad_stats* no_stats = nullptr;
+  AdamwNormArgs norm;  // but for a call's buffers
 };
 
 namespace {
@@ -306,7 +307,24 @@ int build(fr_muon* o) {
     t_gram[i] = gram[i].dealt(Y.recs, Y.side);
     t_whole[i] = whole[i].dealt(Y.recs, Y.side);
   }
+  // the gradients' norm is AdamW's, over tiles of kNormBytes
+  std::vector<AdamwRec> tensors(n);
+  uint64_t norm_slots = 0;
+  const auto norm_tiles = [](const MuonRec& r) { return (r.numel * (r.grad_f32 ? 4 : 2) + kNormBytes - 1) / kNormBytes; };
+  for (uint32_t k = 0; k < n; k++) {
+    std::memset(&tensors[k], 0, sizeof tensors[k]);
+    tensors[k].numel = Y.recs[k].numel;
+    tensors[k].grad = Y.recs[k].grad;
+    tensors[k].grad_f32 = Y.recs[k].grad_f32;
+    norm_slots += norm_tiles(Y.recs[k]);
+  }
+  const uint64_t norm_stride = (norm_slots + 7) / 8;
+  std::vector<uint64_t> norm_walk(8 * norm_stride, 0);
+  for (uint64_t k = 0, g = 0; k < n; k++)
+    for (uint64_t i = 0; i < norm_tiles(Y.recs[k]); i++, g++) norm_walk[(g & 7) * norm_stride + (g >> 3)] = k << 32 | i;
   Carver c;
+  const size_t nt = c.add(tensors.data(), n * sizeof(AdamwRec)), nw = c.add(norm_walk.data(), norm_walk.size() * 8);
+  const size_t nn = c.add(nullptr, (8 * norm_stride + kNormFold) * sizeof(double)), na = c.add(nullptr, kNormArriveBytes);
   const size_t recs = c.add(Y.recs.data(), n * sizeof(MuonRec));
   const fr_grad_stats neutral = {0.0, 0.0f, 1.0f, 0};
   const size_t ns = c.add(&neutral, sizeof neutral);
@@ -339,9 +357,14 @@ int build(fr_muon* o) {
   for (const Carver::Piece& p : c.pieces)
     if (e == hipSuccess && p.src && p.bytes)
       e = hipMemcpyAsync(base + p.at, p.src, p.bytes, hipMemcpyHostToDevice, s);
+  if (e == hipSuccess) e = hipMemsetAsync(at(na), 0, kNormArriveBytes, s);
   const hipError_t es = hipStreamSynchronize(s);
   (void)hipStreamDestroy(s);
   if (e != hipSuccess || es != hipSuccess) return device_error(e != hipSuccess ? e : es);
+  o->norm.recs = reinterpret_cast<const AdamwRec*>(at(nt));
+  o->norm.walk = AdamwWalk{reinterpret_cast<const uint64_t*>(at(nw)), norm_slots, norm_stride};
+  o->norm.parts = reinterpret_cast<double*>(at(nn));
+  o->norm.arrived = reinterpret_cast<uint32_t*>(at(na));
   int units = 0;
   e = hipDeviceGetAttribute(&units, hipDeviceAttributeMultiprocessorCount, o->device);
   if (e != hipSuccess) return device_error(e);
@@ -511,6 +534,22 @@ int check_sums(const fr_muon* o, const fr_chunk_sum* sums) {
 }
 
 }  // namespace
+
+extern "C" int fr_muon_grad_norm(const fr_muon* opt, const void* grads, float max_norm, fr_grad_stats* stats,
+                                 hipStream_t stream) {
+  if (!opt || !stats || !(max_norm > 0)) return FR_E_INVAL;
+  const uint64_t gb = opt->layout.info.grad_arena_bytes;
+  FR_TRY(check_device_and_stream(opt->device, stream));
+  FR_TRY(check_buffer(opt->device, grads, gb, 16));
+  FR_TRY(check_buffer(opt->device, stats, sizeof(fr_grad_stats), 8));
+  const Region outs[] = {{stats, sizeof(fr_grad_stats)}}, ins[] = {{grads, gb}};
+  FR_TRY(check_disjoint(outs, 1, ins, 1));
+  AdamwNormArgs a = opt->norm;
+  a.grads = grads;
+  a.max_norm = max_norm;
+  a.stats = stats;
+  return launch_result(launch_adamw_norm(a, stream));
+}
 
 extern "C" int fr_muon_direction(const fr_muon* opt, void* state, const void* grads, const fr_muon_hyper* hyper,
                                  const fr_grad_stats* stats, void* updates, fr_chunk_sum* sums, hipStream_t stream) {

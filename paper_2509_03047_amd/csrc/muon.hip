@@ -376,13 +376,13 @@ struct ProductArgs {
 
 // How a workgroup makes a tile of B x B elements: waves of WM x WN, S slices
 // of the sum, each D deep, in LDS.
-template <uint32_t B_, uint32_t WM_, uint32_t WN_, uint32_t S_, uint32_t D_>
+template <uint32_t B_, uint32_t WM_, uint32_t WN_, uint32_t S_>
 struct Shape {
-  static constexpr uint32_t B = B_, WM = WM_, WN = WN_, S = S_, D = D_;
+  static constexpr uint32_t B = B_, WM = WM_, WN = WN_, S = S_, D = 64;
   static constexpr uint32_t waves = B / WM * (B / WN), threads = 64 * waves;
 };
-typedef Shape<256, 128, 64, 2, 64> Large;
-typedef Shape<64, 32, 32, 4, 64> Small;
+typedef Shape<256, 128, 64, 2> Large;
+typedef Shape<64, 32, 32, 4> Small;
 
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
@@ -412,9 +412,8 @@ __device__ __forceinline__ uint32_t column_of(uint32_t q, uint32_t lane) {
 // A slice of an operand whose rows run along the sum: B rows of D.  Chunks of
 // 16 bytes are permuted by their row, so that the 16 rows whose chunk is read at
 // one time lie in different banks: rows in turn of L, column_of's of R.
-template <class T, bool kR>
+template <bool kR>
 __device__ __forceinline__ uint32_t row_key(uint32_t row) {
-  if (T::D == 32) return kR ? row / 8 % 4 : row / 4 % 4;
   return kR ? row / 2 % 2 | row / 8 % 4 * 2 : row / 2 % 8;
 }
 // (One offset a lane, of the first of a wave's loads: the others' rows have the
@@ -426,7 +425,7 @@ struct Rows {
   __device__ __forceinline__ Rows(uint32_t wave, uint32_t ld) {
     const uint32_t lane = threadIdx.x % 64, row = wave * kRows + lane / kChunks;
     static_assert(T::waves * kRows % 32 == 0, "keys go by rows mod 32");
-    offset = (row * ld + ((lane % kChunks) ^ row_key<T, kR>(row)) * 8) * 2;
+    offset = (row * ld + ((lane % kChunks) ^ row_key<kR>(row)) * 8) * 2;
   }
   __device__ __forceinline__ void fetch(const f16* src, uint32_t ld, f16* lds, uint32_t wave) const {
 #pragma unroll
@@ -436,7 +435,7 @@ struct Rows {
 };
 template <class T, bool kR>
 __device__ __forceinline__ f16x8 operand_of_row(const f16* lds, uint32_t row, uint32_t chunk) {
-  return *reinterpret_cast<const f16x8*>(lds + row * T::D + (chunk ^ row_key<T, kR>(row)) * 8);
+  return *reinterpret_cast<const f16x8*>(lds + row * T::D + (chunk ^ row_key<kR>(row)) * 8);
 }
 
 // A slice of R where its columns run along the sum: D rows of B.  Chunks are
@@ -711,31 +710,23 @@ __global__ __launch_bounds__(T::threads) void k_muon_product(ProductArgs args) {
     o.multiply(acc, set, 1);
     interleave<Ops::kReadsL + Ops::kReadsR, M * N / 2>();
   };
-  // 64 of the sum, one slice or two, after each of which there may be another to
-  // load (where there is none, the waits are for all)
-  const auto sixty_four = [&](uint32_t k, auto first, auto second, auto last) {
-    const auto next_slice = [&](uint32_t load, auto more) {
+  // A slice, behind which there may be another to load (where there is none, the
+  // wait is for all)
+  const auto one_slice = [&](uint32_t k, auto more, auto last) {
+    first_half(0, 0);
+    second_half(0, 1);
+    first_half(1, 1);
+    if constexpr (last) {
+      o.multiply(acc, 1, 1);
+    } else {
       // the next slice is there, and nobody reads this one any more
       if constexpr (more) {
         arrive<(T::S - 2) * kLoads>();
-        fetch(load);
+        fetch(k + T::S * T::D);
       } else {
         arrive<0>();
       }
       at = following(at);
-    };
-    first_half(0, 0);
-    if constexpr (T::D == 32) {
-      next_slice(k + T::S * 32, first);
-      second_half(0, 0);
-    } else {
-      second_half(0, 1);
-    }
-    first_half(1, T::D == 32 ? 0 : 1);
-    if constexpr (last) {
-      o.multiply(acc, 1, 1);
-    } else {
-      next_slice(k + 64 - T::D + T::S * T::D, second);
       second_half(1, 0);
     }
   };
@@ -825,15 +816,9 @@ __global__ __launch_bounds__(T::threads) void k_muon_product(ProductArgs args) {
       o.read_r(0, at, 0);
       o.read_l(0, at, 0);
       uint32_t k = 0;
-      for (; k + 64 - T::D + T::S * T::D < K; k += 64) sixty_four(k, yes, yes, no);
-      if constexpr (T::D == 32 && T::S % 2 == 1) {
-        if (k + T::S * T::D < K) {
-          sixty_four(k, yes, no, no);
-          k += 64;
-        }
-      }
-      for (; k + 64 < K; k += 64) sixty_four(k, no, no, no);
-      sixty_four(k, no, no, yes);
+      for (; k + T::S * T::D < K; k += T::D) one_slice(k, yes, no);
+      for (; k + T::D < K; k += T::D) one_slice(k, no, no);
+      one_slice(k, no, yes);
     }
 
     const MuonRec* const rec = here.rec;

@@ -192,6 +192,7 @@ def _load():
         "fr_muon_query": [P, u32, u64, u64, P, u32, u32, u64, u64, P, u32, C.POINTER(fr_muon_info)],
         "fr_muon_state_table": [P, u32, u32, u32, P, u32, C.POINTER(u32), P, C.POINTER(u64), C.POINTER(u64),
                                 C.POINTER(u64)],
+        "fr_muon_grad_norm": [P, P, C.c_float, P, P],
         "fr_muon_direction": [P, P, P, P, P, P, P, P],
         "fr_muon_orthogonalize": [P, P, P, P, P],
         "fr_muon_apply": [P, P, P, P, P, P, P],
@@ -236,7 +237,7 @@ EXPORTED = (
     "fr_adamw_create", "fr_adamw_get_info", "fr_adamw_destroy", "fr_adamw_query", "fr_adamw_state_table",
     "fr_grad_norm", "fr_grad_scale", "fr_adamw_step", "fr_adamw_convert",
     "fr_muon_create", "fr_muon_get_info", "fr_muon_destroy", "fr_muon_query", "fr_muon_state_table",
-    "fr_muon_direction", "fr_muon_orthogonalize", "fr_muon_apply",
+    "fr_muon_grad_norm", "fr_muon_direction", "fr_muon_orthogonalize", "fr_muon_apply",
     "fr_embed_create", "fr_embed_get_info", "fr_embed_destroy", "fr_embed_query", "fr_embed_lookup", "fr_embed_grad",
     "fr_tracker_create", "fr_tracker_destroy", "fr_tracker_heartbeat",
     "fr_tracker_report_failure", "fr_tracker_decide", "fr_tracker_failed_ranks", "fr_tracker_donors",
@@ -863,6 +864,9 @@ class Muon:
 
         return torch.empty(max(self.info["update_arena_bytes"], 16), dtype=torch.uint8, device=device)
 
+    def grad_norm(self, grads, max_norm, stats, stream=None):
+        return fr_muon_grad_norm(self, grads, max_norm, stats, stream)
+
     def direction(self, state, grads, hyper, updates, stats=None, sums=None, stream=None):
         return fr_muon_direction(self, state, grads, hyper, updates, stats, sums, stream)
 
@@ -880,6 +884,11 @@ def fr_muon_create(plan: Plan, tensors, n_groups: int, grad_arena_bytes: int, up
 
 def fr_muon_destroy(opt: Muon) -> None:
     opt.destroy()
+
+
+def fr_muon_grad_norm(opt: Muon, grads, max_norm: float, stats, stream=None) -> None:
+    _check(_lib.fr_muon_grad_norm(opt.handle, _dev(grads, opt.info["grad_arena_bytes"], "grads"), max_norm,
+                                  _dev(stats, STATS_BYTES, "stats"), _stream(stream)), "fr_muon_grad_norm")
 
 
 def fr_muon_direction(opt: Muon, state, grads, hyper, updates, stats=None, sums=None, stream=None) -> None:
@@ -967,7 +976,11 @@ class Embedding:
         _check(_lib.fr_embed_get_info(self._h, C.byref(info)), "fr_embed_get_info")
         self.info = info.as_dict()
 
-    handle = Muon.handle
+    @property
+    def handle(self):
+        if self._h is None:
+            raise ValueError("embedding destroyed")
+        return self._h
 
     def destroy(self):
         if self._h is not None:

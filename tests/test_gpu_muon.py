@@ -308,6 +308,44 @@ def test_no_matrices():
     assert (to_host(d.updates) == 0xEE).all()
 
 
+@pytest.mark.parametrize("dtype", [F.FR_BF16, F.FR_F32])
+@pytest.mark.parametrize("shapes", [SHAPES, [(0, 4)], [(3000, 3000)]])
+def test_gradient_norm(dtype, shapes):
+    """Squares are exact in 64 bits, and so many sums of them are off by less than 2^-52 of the whole each in any order."""
+    s = R.Matrices(shapes, dtype, seed=18)
+    d = Dev(s)
+    want = sum(float((s.grad(k).astype(np.float64) ** 2).sum()) for k in range(len(shapes)))
+    n = sum(a * b for a, b in shapes)
+    for _ in range(2):
+        d.stats.fill_(-1)
+        d.opt.grad_norm(d.grads, 1e-2, d.stats)
+        got, norm, scale = float(d.stats[0]), *(float(x) for x in d.stats.view(torch.float32)[2:4])
+        assert abs(got - want) <= n * 2.0 ** -52 * want
+        assert norm == np.float32(np.sqrt(got)) and int(d.stats.view(torch.int64)[2]) == 0
+        assert scale == (np.float32(1e-2) / np.float32(norm) if norm > np.float32(1e-2) else 1.0)
+    g = s.grad(0)
+    if g.size:
+        g[-1] = np.inf
+        s.set_grad(0, g)
+        d.opt.grad_norm(to_dev(s.grads), 1e-2, d.stats)
+        assert int(d.stats.view(torch.int64)[2]) == 1 and float(d.stats.view(torch.float32)[3]) == 0.0
+
+
+def test_gradient_norm_refusals():
+    s = R.Matrices([(5, 7), (64, 64)], F.FR_F32)
+    d = Dev(s)
+    lib, o, st = F._lib, d.opt.handle, torch.cuda.current_stream().cuda_stream
+    g, t = d.grads.data_ptr(), d.stats.data_ptr()
+    for args, want in (((o, g, 0.0, t, st), -1), ((o, g, float("nan"), t, st), -1), ((o, g, 1.0, None, st), -1),
+                       ((o, g + 8, 1.0, t, st), -2), ((o, g, 1.0, t + 4, st), -2)):
+        assert lib.fr_muon_grad_norm(*args) == want, args
+    assert lib.fr_muon_grad_norm(o, g, 1.0, g + 16, st) < 0  # the statistics lie in the gradients
+    with pytest.raises(ValueError):
+        d.opt.grad_norm(d.grads[:-16], 1.0, d.stats)
+    torch.cuda.synchronize()
+    assert np.array_equal(to_host(d.grads), s.grads)
+
+
 # ---------------------------------------------------------- streams, graphs
 
 

@@ -43,7 +43,7 @@ class Replica:
         self.state = torch.zeros(m.arena_bytes, dtype=torch.uint8, device="cuda")
         self.grads = torch.zeros(m.grad_bytes, dtype=torch.uint8, device="cuda")
         self.updates, self.sums = m.muon.empty_updates().zero_(), m.plan.empty_sums().zero_()
-        self.stats = m.adamw.empty_stats().zero_()
+        self.stats, self.mat_stats = (m.adamw.empty_stats().zero_() for _ in range(2))
         self.x = torch.zeros(TOKENS, D, dtype=torch.bfloat16, device="cuda")
         self.ids = torch.zeros(TOKENS, dtype=torch.int64, device="cuda")
         gen = torch.Generator().manual_seed(seed)
@@ -81,6 +81,9 @@ class Replica:
         dx = (dh @ a.t().contiguous()).to(torch.bfloat16)
         m.emb.grad(self.ids, dx, self.grads)
         m.adamw.grad_norm(self.grads, 1.0, self.stats)
+        m.muon.grad_norm(self.grads, 1.0, self.mat_stats)
+        self.stats[0] += self.mat_stats[0]  # over all tensors
+        m.adamw.grad_scale(1.0, self.stats)
         m.muon.direction(self.state, self.grads, hyper[1], self.updates, self.stats, self.sums)
         m.muon.apply(self.state, self.updates, hyper[1], self.stats, self.sums)
         m.adamw.step(self.state, self.grads, hyper[0], self.stats, self.sums)
@@ -140,6 +143,7 @@ def test_captured_steps_are_the_eager_ones():
         r.m.emb.lookup(r.state, ids, r.x)
         r.m.emb.grad(ids, dx, r.grads)
         r.m.adamw.grad_norm(r.grads, 1.0, r.stats)
+        r.m.muon.grad_norm(r.grads, 1.0, r.mat_stats)
         r.m.muon.direction(r.state, r.grads, h[1], r.updates, r.stats, r.sums)
         r.m.muon.apply(r.state, r.updates, h[1], r.stats, r.sums)
         r.m.adamw.step(r.state, r.grads, h[0], r.stats, r.sums)

@@ -126,6 +126,7 @@ def test_null_pointers():
     assert L.fr_muon_get_info(None, None) == INVAL and L.fr_muon_destroy(None) == 0
     assert L.fr_muon_query(None, 0, 4096, 0, None, 0, 0, 0, 0, None, 0, None) == INVAL
     assert L.fr_muon_direction(None, None, None, None, None, None, None, None) == INVAL
+    assert L.fr_muon_grad_norm(None, None, 1.0, None, None) == INVAL
     assert L.fr_muon_orthogonalize(None, None, None, None, None) == INVAL
     assert L.fr_muon_apply(None, None, None, None, None, None, None) == INVAL
     assert L.fr_embed_create(None, None, 0, None) == INVAL
