@@ -663,9 +663,9 @@ int fr_adamw_convert(const fr_adamw* from, const void* from_state, const fr_adam
  *     and fp32 sums; X has up to four bits more while three or more steps are to
  *     come, and what fp16 leaves of the diagonals of A and of its polynomials is
  *     kept and counted.  Updates are then off by some 1.8e-3 of their norm (those
- *     of a few elements up to 3e-3), of which the rounding to bf16 makes 1.7e-3.  U depends on D, eps and the
- *     coefficients alone, not on the other matrices nor on the launch: replicas
- *     stay identical bit for bit.
+ *     of a few elements up to 3e-3), of which the rounding to bf16 makes 1.7e-3.
+ *     U depends on D, eps and the coefficients alone, not on the other matrices
+ *     nor on the launch: replicas stay identical bit for bit.
  *     A matrix of zeros gives zeros (eps > 0); one that holds a NaN or an
  *     infinity gives NaN everywhere; other matrices do not feel it.
  *   Step, rounded operation by operation like AdamW's, with the matrix's scale:

@@ -84,6 +84,10 @@ int check_coeffs(const fr_muon_coeffs* c, uint32_t n, std::vector<fr_muon_coeffs
 }
 
 // Which tiles the products take, and where in the scratch their operands lie.
+// Large ones from 256 on, one for each compute unit.  Large and small, us: of 1024 x
+// 1024 matrices 64 tiles 524 and 313, 128 544 and 506, 192 564 and 688, 256 586 and
+// 874, 512 1,197 and 1,713; of 2048 x 4096 128 tiles 1,055 and 674, 256 1,121 and
+// 1,129, 384 1,349 and 1,630; one of 4096 x 4096, 256 tiles, 1,623 and 2,642.
 void lay_out_scratch(MuonLayout* out) {
   uint64_t large = 0;
   for (const MuonRec& r : out->recs) {
@@ -92,7 +96,7 @@ void lay_out_scratch(MuonLayout* out) {
   }
   out->side = large >= 256 ? kMuonLarge : kMuonSmall;
   for (MuonRec& r : out->recs) {
-    r.paired = out->pair && r.m >= kMuonPairedLess && r.n >= kMuonPairedMore;
+    r.paired = out->pair && r.m >= kMuonPairedLess && r.n >= kMuonPairedMore && r.n >= kMuonPairedRatio * r.m;
     r.mp = uint32_t(up(r.m, out->side));
     r.np = uint32_t(up(r.n, out->side));
     if (!r.numel) continue;

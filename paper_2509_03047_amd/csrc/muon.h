@@ -38,9 +38,14 @@ constexpr uint32_t kMuonTile = 4096, kMuonSub = 1024;
 static_assert(kMuonSub * 4 <= FR_ADAMW_MIN_SUM_CHUNK, "a sub-tile lies inside a chunk");
 // Sides of the products' tiles, to which those of matrices are padded.
 constexpr uint32_t kMuonLarge = 256, kMuonSmall = 64;
-// Matrices whose first two steps are taken as one: five products of square
-// matrices more and one gram and one product with X less.
-constexpr uint32_t kMuonPairedLess = 128, kMuonPairedMore = 2048;
+// Matrices whose first two steps are taken as one: 3 m^3 / 2 multiplications more
+// and 3 m^2 n / 2 fewer, in three launches more.  As one and one by one, us: 8 of 128 x 1024 102 and 99, of 128 x 2048 132
+// and 134, of 128 x 4096 181 and 201, 4 of 512 x 2048 182 and 190, 32 of 1024 x 2048
+// 1,899 and 1,952, 3 of 2048 x 4096 1,350 and 1,377 (but 2 of them 1,121 and 1,101);
+// one of 4096 x 4096 1,624 and 1,537, 32 of 2048 x 2048 6,660 and 6,370, of 1024 x
+// 1024 1,303 and 1,198.  (8 of 64 x 4096 157 and 170, but fewer elements average out
+// what the missing gram does not mend.)
+constexpr uint32_t kMuonPairedLess = 128, kMuonPairedMore = 2048, kMuonPairedRatio = 2;
 constexpr float kMuonLiftA = 256.0f;  // A and Q are stored times this
 
 // A product's work, one entry for each workgroup: a tile of a matrix, of which it
