@@ -7,7 +7,16 @@
 // by wave; a second pass puts each token at its place.  Its waves have
 // consecutive tokens, so the order within a row is the tokens' own, and nothing
 // depends on atomics' order.  A row of more than FR_EMBED_RUN tokens is cut into
-// runs, which a launch of their own sums up; the last launch writes the rows.
+// runs: the second launch sums those up and writes the shorter rows, the third adds
+// up the runs of the long ones.
+//
+// What bounds them: HBM, and where there are few tokens the launches.  16,384
+// tokens of 4,096 columns, a share of 16,032 rows of the vocabulary, bf16: a lookup
+// takes 29 us when called again and again (168 MB, 5.8 TB/s, in part from the
+// Infinity Cache; 47 with other rows in between), the order 17 us (two walks over the ids and what
+// hangs on them in turn), rows and runs 33 us (177 MB, 5.4 TB/s), the long rows 5 us.
+// 2,048 tokens of 256 columns: 9, 10 and 3 us, each of them a launch and a few
+// loads that wait for each other.
 #include <hip/hip_runtime.h>
 
 #include "embed.h"
@@ -369,6 +378,14 @@ __global__ __launch_bounds__(256) void k_embed_long(EmbedArgs a, Units units, ui
   write_row<kGrad32>(a, row, v, span);
 }
 
+// Above so many slices of rows, some four times the waves that the card holds, a unit
+// of k_embed_rows takes two.  Two and one, us: 16,384 tokens, 16,032 rows of 1,024
+// columns (32,064 slices) 40 and 37, of 1,536 41 and 43, of 2,048 44 and 48, of 4,096
+// 67 and 75, 128,256 rows of 1,024 87 and 104; 4,096 tokens, 8,192 rows of 2,048
+// (32,768) 30 and 26, of 4,096 both 34; 65,536 tokens, 2,000 rows of 2,048 (8,000)
+// 119 and 111.
+constexpr uint32_t kTwoSlices = 32768;
+
 // Units of up to 64 lanes: one for up to 512 columns.
 Units units_of(uint32_t cols) {
   Units u;
@@ -406,7 +423,7 @@ int launch_embed_grad(const EmbedArgs& a, void* stream) {
   hipLaunchKernelGGL(k_embed_order, dim3(1u << log), dim3(64 * kEmbedWaves), 0, st, a, log, R, bits);
   if (const int e = int(hipGetLastError())) return e;
   const Units u = units_of(a.cols);
-  const uint32_t U = u.slices > 1 ? 2 : 1, row_slices = (u.slices + U - 1) / U;
+  const uint32_t U = u.slices > 1 && uint64_t(a.rows) * u.slices > kTwoSlices ? 2 : 1, row_slices = (u.slices + U - 1) / U;
   const uint32_t runs = a.n > kRun ? uint32_t(embed_run_slots(a.n) * u.slices) : 0, all = runs + a.rows * row_slices;
   const auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3(blocks_of(all, u)), dim3(256), 0, st, a, u, runs, row_slices, all);

@@ -1,6 +1,21 @@
 // gfx950 kernels of the step by orthogonalised momentum: the momenta and norms
 // of all matrices of a state, the products that orthogonalise them, and the
 // step along the updates.
+//
+// X <- a X + (b A + c A A) X with A = X X^T is three launches a step over all
+// matrices: A, Q = b A + c A A, and a X + Q X.  A and Q are symmetric: of them
+// only tiles on and below the diagonal are multiplied, and mirrored.  The smaller
+// side is A's (X of a tall matrix is its transpose).
+//
+// What bounds them, in the share of an 8B model (0.87e9 elements in 224 matrices,
+// 22.8 TFLOP, 26.5 ms; a large library product of fp16 reaches 1.3 PFLOP/s here): a
+// gram takes 1.38 ms, the level of that product; a X + Q X 2.9 ms, 0.9 PFLOP/s, as
+// reading and writing X by tiles is not hidden behind the matrix instructions of
+// these shorter sums (of 5.7 M cycles 4.0 M are left without it); a square
+// product 0.75 to 0.88 ms.  Momenta and norms take 1.45 ms and X_0 1.58, the step 1.75
+// (10.5 GB, 6.0 TB/s) and with sums 1.77: HBM.  Of eight matrices of 256 x 256 to
+// 256 x 1024 a product takes 5 to 9 us and all 122: a chain of launches, whose
+// workgroups' loads wait for each other.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -303,7 +318,10 @@ __device__ __forceinline__ f32x4 spread_four(const MuonArgs& a, const MuonRec& r
   return d;
 }
 
-// kNorms: every workgroup takes its matrix's factor from the tiles' sums itself.
+// kNorms: every workgroup takes its matrix's factor from the tiles' sums itself, a
+// launch less, where no matrix has more of them than a workgroup threads.  (With the
+// launch and without, us: eight matrices of 64 sums 139.5 and 137.3, of 256 510.7 and
+// 508.2; of 1,024 1,043 and 1,052.)
 template <bool kNorms>
 __global__ __launch_bounds__(256) void k_muon_spread(MuonArgs a) {
   if (a.stats->nonfinite) return;
@@ -381,6 +399,12 @@ struct Shape {
   static constexpr uint32_t B = B_, WM = WM_, WN = WN_, S = S_, D = 64;
   static constexpr uint32_t waves = B / WM * (B / WN), threads = 64 * waves;
 };
+// Large: one workgroup a compute unit (128 KB of slices, 32 of mirrors); a
+// wave reads 12 KB of operands for 32 matrix instructions.  (Four waves of 128 x 128
+// took 3.3 ms of the share's a X + Q X where eight took 3.03, for copies of sums
+// between register files; four or five slices of 32 in turn no less than two of 64.)
+// Small: two workgroups a compute unit (72 KB each), four slices for what little there is of
+// a sum.
 typedef Shape<256, 128, 64, 2> Large;
 typedef Shape<64, 32, 32, 4> Small;
 

@@ -128,6 +128,14 @@ def test_gradient(rows, cols, n, kind, dout, grad, add):
         assert e.around()
 
 
+@pytest.mark.parametrize("rows,cols,n,kind", [(16385, 515, 3000, "zipf"), (16384, 515, 3000, "zipf"),
+                                              (10923, 1040, 700, "zipf"), (32769, 513, 200, "any"), (8200, 2055, 65, "one")])
+@pytest.mark.parametrize("dout,grad,add", [("bf16", "f32", False), ("f32", "bf16", True)])
+def test_gradient_of_many_rows(rows, cols, n, kind, dout, grad, add):
+    """On both sides of what a unit takes of a row, with slices that its end cuts off."""
+    test_gradient(rows, cols, n, kind, dout, grad, add)
+
+
 def test_gradient_in_64_bits():
     """Sums of n terms of fp32 in runs: at most about 3 * 64 roundings of 2^-24 of the terms' sum of magnitudes, and a
     product's."""
