@@ -9,7 +9,8 @@
 //
 // What bounds them, in the share of an 8B model (0.87e9 elements in 224 matrices,
 // 22.8 TFLOP, 26.5 ms; a large library product of fp16 reaches 1.3 PFLOP/s here): a
-// gram takes 1.38 ms, the level of that product; a X + Q X 2.9 ms, 0.9 PFLOP/s, as
+// gram takes 1.38 ms (1.16 PFLOP/s with padding and whole tiles on the diagonal,
+// where a library's batch of such products reaches 1.12); a X + Q X 2.9 ms, 0.9, as
 // reading and writing X by tiles is not hidden behind the matrix instructions of
 // these shorter sums (of 5.7 M cycles 4.0 M are left without it); a square
 // product 0.75 to 0.88 ms.  Momenta and norms take 1.45 ms and X_0 1.58, the step 1.75
