@@ -731,8 +731,12 @@ typedef struct fr_muon_info {
  *             NULL, with n_steps = 0: five of (3.4445, -4.7750, 2.0315)
  * Errors as of fr_adamw_create; FR_E_INVAL also for rows * cols other than the
  * master's numel, a scale that is not finite, and coefficients that are not
- * finite or let a singular value in [0, 1] grow past 4, or |b s^2| + |c s^4|
- * past 64, on the way; FR_E_RANGE for a side of more than 2^20 or 2^31 elements
+ * finite; that let a singular value in [0, 1] grow past 4, or |b s^2| + |c s^4|
+ * past 64, on the way; that do so past 8 or 128 for some value that roundings may
+ * leave (up to 1 + 2^-10 at first, and in each step up to 2^-10 of itself more than
+ * any value before it can give); or whose slopes let errors of 2^-11 of a value in
+ * each step come to more than 4.  (Steps that are made for [0, 1] to the last bit
+ * need room: a / 1.01, b / 1.01^3, c / 1.01^5.)  FR_E_RANGE for a side of more than 2^20 or 2^31 elements
  * or more, a smaller side above 2^15, and for 2^34 elements in all, those of a
  * matrix counted in whole 4,096s, or 2^35 with sides rounded up to 64;
  * FR_E_OVERLAP also for two updates that overlap.

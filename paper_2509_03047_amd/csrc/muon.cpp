@@ -53,9 +53,22 @@ int check_shape(uint64_t rows, uint64_t cols) {
   return FR_OK;
 }
 
+// What operands' roundings may do to a singular value in a step, of itself: as a
+// unit half a step of fp16, and twice that where range is at stake.
+constexpr double kUnit = 1.0 / 2048, kMargin = 2 * kUnit;
+
 // Whether the steps keep every singular value that starts in [0, 1], and the
 // polynomial's parts, inside what fp16 operands can hold with the powers of two
-// that they are stored times.
+// that they are stored times; and so that it holds for the values that roundings
+// leave, not for exact ones alone:
+//   * up to 4 and 64 exactly, up to 8 and 128 where everything that a step may
+//     leave is up to kMargin larger (of 16 and 256, where A and Q pass fp16's
+//     range).  Steps made for [0, 1] and no further, with a slope of 12 at its end,
+//     leave values of 1e21 so.
+//   * errors of kUnit in each step come to 4 at most in the last X, by the slopes
+//     of the steps behind them: to 0.014 with kCoeffs, 0.12 with steps that start
+//     with a slope of 8, 2.1 with kCoeffs 16 times; 50,000 with 16 steps that each
+//     tear neighbours apart.
 // *pair: those of the first two steps taken as one as well.
 int check_coeffs(const fr_muon_coeffs* c, uint32_t n, std::vector<fr_muon_coeffs>* out, bool* pair) {
   if (!c && n) return FR_E_INVAL;
@@ -66,8 +79,9 @@ int check_coeffs(const fr_muon_coeffs* c, uint32_t n, std::vector<fr_muon_coeffs
     if (!std::isfinite(k.a) || !std::isfinite(k.b) || !std::isfinite(k.c)) return FR_E_INVAL;
   *pair = out->size() >= 2;
   constexpr int kGrid = 4096;
+  // (compared so that an overflow is a refusal)
   for (int i = 0; i <= kGrid; i++) {
-    double s = double(i) / kGrid;
+    double s = double(i) / kGrid, error = kUnit * s;
     if (*pair) {
       const fr_muon_coeffs &f = (*out)[0], &g = (*out)[1];
       const double q = s * s, one = f.b * q + f.c * q * q, p = q * (f.a + one) * (f.a + one), two = g.b * p + g.c * p * p;
@@ -75,10 +89,24 @@ int check_coeffs(const fr_muon_coeffs* c, uint32_t n, std::vector<fr_muon_coeffs
     }
     for (const fr_muon_coeffs& k : *out) {
       const double q = s * s;
-      if (std::fabs(k.b) * q + std::fabs(k.c) * q * q > 64) return FR_E_INVAL;
+      if (!(std::fabs(k.b) * q + std::fabs(k.c) * q * q <= 64)) return FR_E_INVAL;
+      error *= std::fabs(k.a + 3 * k.b * q + 5 * k.c * q * q);
       s *= k.a + k.b * q + k.c * q * q;
       if (!(std::fabs(s) <= 4)) return FR_E_INVAL;
+      error += kUnit * std::fabs(s);
     }
+    if (!(error <= 4)) return FR_E_INVAL;
+  }
+  double top = 1 + kMargin;  // everything up to here may come
+  for (const fr_muon_coeffs& k : *out) {
+    if (!(std::fabs(k.b) * top * top + std::fabs(k.c) * top * top * top * top <= 128)) return FR_E_INVAL;
+    double next = 0;
+    for (int i = 1; i <= kGrid; i++) {
+      const double s = top * i / kGrid, q = s * s;
+      next = std::max(next, std::fabs(s * (k.a + k.b * q + k.c * q * q)));
+    }
+    top = next * (1 + kMargin);
+    if (!(top <= 8)) return FR_E_INVAL;
   }
   return FR_OK;
 }
