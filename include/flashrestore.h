@@ -660,10 +660,17 @@ int fr_adamw_convert(const fr_adamw* from, const void* from_state, const fr_adam
  *     steps; the update U is the last X in bf16.  On singular values a step is
  *     the polynomial a s + b s^3 + c s^5.  The sum of squares is kept in 64 bits;
  *     products have fp16 operands (a power of two brings them into its range)
- *     and fp32 sums; X has up to four bits more while three or more steps are to
- *     come, and what fp16 leaves of the diagonals of A and of its polynomials is
- *     kept and counted.  Updates are then off by some 1.8e-3 of their norm (those
- *     of a few elements up to 3e-3), of which the rounding to bf16 makes 1.7e-3.
+ *     and fp32 sums; X has eight bits more while three or more steps are to come,
+ *     and what fp16 leaves of the diagonals of A and of its polynomials is kept and
+ *     counted.  Of their norm, updates by the default steps are then off, the
+ *     rounding to bf16 of 1.7e-3 among it, by
+ *       up to 2.5e-3 where singular values are spread, mostly 1.8e-3 to 2.0e-3;
+ *       up to 3.5e-3 where some are 1,000 times the others or more (low rank):
+ *         the steps multiply small directions by up to 3.4445^5 = 485, and with them
+ *         what roundings leave there;
+ *       up to 5e-3 for matrices of a few elements, up to 1.5e-2 where all elements,
+ *         or all singular values but zeros, are equal: roundings do not average out.
+ *     Other steps pass roundings on by slopes of their own.
  *     U depends on D, eps and the coefficients alone, not on the other matrices
  *     nor on the launch: replicas stay identical bit for bit.
  *     A matrix of zeros gives zeros (eps > 0); one that holds a NaN or an

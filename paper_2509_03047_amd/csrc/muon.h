@@ -13,7 +13,7 @@ namespace fr {
 // and np the same in whole tiles.  Offsets in bytes: of the state, the arenas
 // and, for what the products read and write, the optimizer's scratch:
 //   x     mp x np, fp16    X, twice: read and written in turn
-//   rest  mp x np, 8 bits  what X is more than its fp16 number (e4m3)
+//   rest  mp x np, 8 bits  what X is more than its fp16 number, in 2^-8 of its last place
 //   square    mp x mp, fp16   X X^T and polynomials of it, three at a time
 //   diagonal  mp, fp32        what their diagonals are more
 struct alignas(16) MuonRec {
