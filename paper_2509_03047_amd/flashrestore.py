@@ -919,17 +919,21 @@ def fr_muon_apply(opt: Muon, state, updates, hyper, stats=None, sums=None, strea
                               _stream(stream)), "fr_muon_apply")
 
 
-def _rows2d(x, n: int, cols: int, name: str):
-    """(address, dtype, elements from row to row) of a device tensor of n rows of
-    cols bf16 or fp32 elements, the elements of a row next to each other."""
+def _rows2d(x, ids, cols: int, name: str):
+    """(address, dtype, elements from row to row) of a device tensor of a row of
+    cols bf16 or fp32 elements for each of ids, in their shape or behind one
+    another, the elements of a row next to each other."""
     import torch
 
-    if not x.is_cuda:
-        raise ValueError(f"{name}: not a device tensor")
+    n = ids.numel()
     if x.dtype not in (torch.float32, torch.bfloat16):
         raise ValueError(f"{name}: {x.dtype}, not float32 or bfloat16")
-    if x.dim() < 2 or x.shape[-1] != cols or x.numel() != n * cols:
-        raise ValueError(f"{name}: shape {tuple(x.shape)} for {n} rows of {cols}")
+    if tuple(x.shape) not in ((*ids.shape, cols), (n, cols)):
+        raise ValueError(f"{name}: shape {tuple(x.shape)} for rows of {cols} of ids of shape {tuple(ids.shape)}")
+    if not x.is_cuda:
+        raise ValueError(f"{name}: not a device tensor")
+    if x.dim() == 1:
+        x = x.unsqueeze(0)
     if n and x.dim() > 2:
         try:
             x = x.view(n, cols)
@@ -1001,9 +1005,10 @@ class Embedding:
 
 
 def _embed_desc(entry, rows, cols, max_tokens, first, grad_dtype, grad_offset):
-    for name, x, top in (("rows", rows, 1 << 32), ("cols", cols, 1 << 32), ("max_tokens", max_tokens, 1 << 64),
-                         ("grad_offset", grad_offset, 1 << 64)):
-        if not 0 <= x < top:
+    for name, x, low, top in (("rows", rows, 0, 1 << 32), ("cols", cols, 0, 1 << 32), ("max_tokens", max_tokens, 0, 1 << 64),
+                              ("grad_offset", grad_offset, 0, 1 << 64), ("entry", entry, -(1 << 31), 1 << 31),
+                              ("first", first, -(1 << 63), 1 << 63)):
+        if not low <= x < top:
             raise ValueError(f"{name}: {x}")
     return fr_embed_desc(grad_offset, first, max_tokens, rows, cols, entry, grad_dtype)
 
@@ -1027,10 +1032,11 @@ def fr_embed_destroy(e: Embedding) -> None:
 
 
 def fr_embed_lookup(e: Embedding, state, ids, out, scale: float = 1.0, stream=None) -> None:
-    """out (of ids' shape and a last dimension of cols, bf16 or fp32; rows may be
-    further apart than cols) <- scale * the rows of ids (int32 or int64)."""
+    """out (of ids' shape and a last dimension of cols, or all rows in two
+    dimensions; bf16 or fp32; rows may be further apart than cols) <- scale * the
+    rows of ids (int32 or int64)."""
+    q, dtype, stride = _rows2d(out, ids, e.info["cols"], "out")
     p, size, n = _ids_of(ids)
-    q, dtype, stride = _rows2d(out, n, e.info["cols"], "out")
     _check(_lib.fr_embed_lookup(e.handle, _dev(state, e.info["arena_bytes"], "state"), p, size, n, scale, q, dtype,
                                 stride, _stream(stream)), "fr_embed_lookup")
 
@@ -1038,8 +1044,8 @@ def fr_embed_lookup(e: Embedding, state, ids, out, scale: float = 1.0, stream=No
 def fr_embed_grad(e: Embedding, ids, dout, grads, scale: float = 1.0, add: bool = False, stream=None) -> None:
     """The embedding's gradient in the arena `grads` <- (add: += ) that of dout,
     which is as `out` of a lookup."""
+    q, dtype, stride = _rows2d(dout, ids, e.info["cols"], "dout")
     p, size, n = _ids_of(ids)
-    q, dtype, stride = _rows2d(dout, n, e.info["cols"], "dout")
     _check(_lib.fr_embed_grad(e.handle, p, size, n, q, dtype, stride, scale,
                               _dev(grads, e.info["grad_arena_bytes"], "grads"), int(bool(add)), _stream(stream)),
            "fr_embed_grad")
