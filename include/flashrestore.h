@@ -724,9 +724,10 @@ typedef struct fr_muon_info {
   uint64_t sums_chunks;        /* chunks whose sums direction and apply write */
   uint64_t device_bytes;       /* device memory of the optimizer itself: 5 bytes for
                                   each element and 6 for each of the smaller
-                                  sides' squares, sides rounded up to 64 (256 for
-                                  256 or more tiles of 256 x 256 in all) (0 for a
-                                  query) */
+                                  sides' squares, sides rounded up to 64, or to 256
+                                  where matrices of 2^24 elements in all need at most
+                                  half the multiplications more so; also where it is
+                                  used for norms and steps alone (0 for a query) */
   int64_t device;              /* -1 for a query */
 } fr_muon_info;
 

@@ -111,18 +111,40 @@ int check_coeffs(const fr_muon_coeffs* c, uint32_t n, std::vector<fr_muon_coeffs
   return FR_OK;
 }
 
-// Which tiles the products take, and where in the scratch their operands lie.
-// Large ones from 256 on, one for each compute unit.  Large and small, us: of 1024 x
-// 1024 matrices 64 tiles 524 and 313, 128 544 and 506, 192 564 and 688, 256 586 and
-// 874, 512 1,197 and 1,713; of 2048 x 4096 128 tiles 1,055 and 674, 256 1,121 and
-// 1,129, 384 1,349 and 1,630; one of 4096 x 4096, 256 tiles, 1,623 and 2,642.
-void lay_out_scratch(MuonLayout* out) {
-  uint64_t large = 0;
-  for (const MuonRec& r : out->recs) {
-    const uint64_t m = (r.m + kMuonLarge - 1) / kMuonLarge, n = (r.n + kMuonLarge - 1) / kMuonLarge;
-    large += r.numel ? m * n : 0;
+// Multiplications of a step of all matrices in tiles of this side, symmetric
+// products by tiles on and below the diagonal.
+double in_tiles(const std::vector<MuonRec>& recs, uint32_t side) {
+  double sum = 0;
+  for (const MuonRec& r : recs) {
+    if (!r.numel) continue;
+    const double m = double(up(r.m, side)), n = double(up(r.n, side));
+    sum += (m + side) * m / 2 * (m + n) + m * m * n;
   }
-  out->side = large >= 256 ? kMuonLarge : kMuonSmall;
+  return sum;
+}
+
+// Which tiles the products take, and where in the scratch their operands lie.
+// Large ones where the matrices have the elements of 256, one for each compute unit,
+// and rounding their sides up costs no more than half the multiplications again
+// (which is what large tiles are faster by).  Large and small, us:
+//   by elements, of 1024 x 1024 matrices those of 64 tiles 524 and 313, of 128 544
+//     and 506, of 192 564 and 688, of 256 586 and 874, of 512 1,197 and 1,713; of 2048 x
+//     4096 128 1,055 and 674, 256 1,121 and 1,129, 384 1,349 and 1,630; one of 4096 x
+//     4096 1,623 and 2,642; 20 of 900 x 900 (247 tiles' elements in 320 tiles) 769 and
+//     970; 40 of 200 to 1,400 (201 in 274) 764 and 595;
+//   by multiplications, times those in small tiles: 1.3 256 of 256 x 256 399 and 514;
+//     1.4 8 of 1100 x 2100 969 and 976; 1.45 90 of 700 x 700 1,809 and 2,064; 1.55 16 of
+//     512 x 4096 with 32 of 128 x 4096 1,146 and 981; 1.6 30 of 1300 x 1300 2,979 and
+//     3,443; 1.75 300 of 448 x 448 2,074 and 2,362, 4 of 2048 x 2048 with 100 of 16 x 4096
+//     2,141 and 1,697; 1.9 100 of 600 x 600 1,836 and 1,787; 2.1 4 of 2048 x 2048 with 1,500
+//     of 64 x 64 3,197 and 1,517; 2.7 600 of 384 x 384 4,016 and 3,369; 4.7 64 of 128 x 4096
+//     1,012 and 458; 64 4,096 of 64 x 64 5,691 and 508.
+void lay_out_scratch(MuonLayout* out) {
+  uint64_t elements = 0;
+  for (const MuonRec& r : out->recs) elements += r.numel;
+  const bool large = elements >= uint64_t(256) * kMuonLarge * kMuonLarge &&
+                     in_tiles(out->recs, kMuonLarge) <= 1.5 * in_tiles(out->recs, kMuonSmall);
+  out->side = large ? kMuonLarge : kMuonSmall;
   for (MuonRec& r : out->recs) {
     r.paired = out->pair && r.m >= kMuonPairedLess && r.n >= kMuonPairedMore && r.n >= kMuonPairedRatio * r.m;
     r.mp = uint32_t(up(r.m, out->side));
