@@ -673,6 +673,10 @@ int fr_adamw_convert(const fr_adamw* from, const void* from_state, const fr_adam
  *     Other steps pass roundings on by slopes of their own.
  *     U depends on D, eps and the coefficients alone, not on the other matrices
  *     nor on the launch: replicas stay identical bit for bit.
+ *     Of a part of a matrix, as a tensor-parallel rank's share is one, U is the
+ *     update of that part by itself, not the part of the whole matrix's: who wants
+ *     that brings the matrix together first, lets ranks orthogonalise whole
+ *     matrices in turn and exchanges the updates before fr_muon_apply.
  *     A matrix of zeros gives zeros (eps > 0); one that holds a NaN or an
  *     infinity gives NaN everywhere; other matrices do not feel it.
  *   Step, rounded operation by operation like AdamW's, with the matrix's scale:

@@ -13,8 +13,10 @@
 // where a library's batch of such products reaches 1.12); a X + Q X 2.9 ms, 0.9, as
 // reading and writing X by tiles is not hidden behind the matrix instructions of
 // these shorter sums (of 5.7 M cycles 4.0 M are left without it); a square
-// product 0.75 to 0.88 ms.  Momenta and norms take 1.45 ms and X_0 1.58, the step 1.75
-// (10.5 GB, 6.0 TB/s) and with sums 1.77: HBM.  Of eight matrices of 256 x 256 to
+// product 0.75 to 0.88 ms.  Momenta and norms take 1.45 ms, the step 1.75 (10.5 GB, 6.0
+// TB/s) and with sums 1.77: HBM.  X_0 takes 1.53 ms (7.9 GB, 5.1 TB/s): its loads stand
+// in branches, so that those of a thread's four parts, the gradient's and the
+// momentum's of each, are waited for one after another.  Of eight matrices of 256 x 256 to
 // 256 x 1024 a product takes 5 to 9 us and all 122: a chain of launches, whose
 // workgroups' loads wait for each other.
 #include <hip/hip_runtime.h>
@@ -166,7 +168,7 @@ __global__ __launch_bounds__(256) void k_muon_momentum(MuonArgs a) {
 }
 
 // One tile of the step, or with U = 1 (where nothing is summed) one sub-tile: an 8B
-// model's share takes 1.63 ms by sub-tiles and 1.78 by tiles, with sums 1.78 by tiles
+// model's share takes 1.75 ms by sub-tiles and 1.80 by tiles, with sums 1.78 by tiles
 // and 2.1 by sub-tiles.
 template <uint32_t U, bool kFull>
 __device__ __forceinline__ void apply_tile(const Elements& t, const MuonArgs& a) {

@@ -62,3 +62,26 @@ def test_steps_with_little_room_near_rank_one():
         # the top value's own rounding, which varies with the order of sums, is passed on by slopes of up to 12: to 0.12
         # were it half a step of fp16 each time; a mean over 64 elements or more leaves an eighth of that at most
         assert M.off(u, want) <= 0.12 / 8, name
+
+
+def test_whole_matrices_of_a_layer():
+    """Not a rank's shares: matrices of 4,096 x 14,336 either way up, and square."""
+    shapes = [(4096, 14336), (14336, 4096), (4096, 4096)]
+    t, rows, ab, gb, ub = F.fr_muon_state_table(shapes)
+    opt = F.Muon(F.Plan(t, 1 << 20, ab, ab), rows, 1, gb, ub)
+    gen = torch.Generator(device="cuda").manual_seed(42)
+    grads = (torch.randn(gb // 2, generator=gen, device="cuda") * 1e-3).to(torch.bfloat16)
+    u = opt.empty_updates()
+    opt.orthogonalize(grads.view(torch.uint8), torch.from_numpy(F.muon_hyper([dict(lr=0.0)]).view(np.uint8)).cuda(), u)
+    for k, (a, b) in enumerate(shapes):
+        x = grads[int(rows[k]["grad_offset"]) // 2:][: a * b].view(a, b).double()
+        got = u[int(rows[k]["update_offset"]):][: 2 * a * b].view(torch.bfloat16).view(a, b)
+        x = x.t().contiguous() if a > b else x
+        got = (got.t().contiguous() if a > b else got).double()
+        x = x / (torch.linalg.norm(x) + 1e-7)
+        for ca, cb, cc in np.asarray(R.STEPS, np.float32).astype(np.float64).tolist():
+            m = x @ x.t().contiguous()
+            x = ca * x + (cb * m + cc * (m @ m)) @ x
+        e = float(torch.linalg.norm(got - x) / torch.linalg.norm(x))
+        log((a, b), f"{e:.2e}")
+        assert e <= M.KINDS["spread"][0], (a, b)
